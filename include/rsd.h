@@ -5,6 +5,10 @@
  *                 rsd_sbs_step            one level of Stochastic Beam Search
  *   verification  rsd_verify_tree         recursive rejection sampling along the draft tree
  *                 rsd_resample_residual   draw from a residual distribution on its own
+ *   scoring       rsd_token_logprobs      log-probabilities of given tokens, entropy, likeliest tokens of rows
+ *                 rsd_emitted_logprobs    the same for the tokens that a verification emitted
+ *                 rsd_row_divergence      KL both ways and overlap of draft and target rows
+ *                 ..._backward            gradients of these with respect to the rows
  *
  * The draft and target language models are outside this library: their logits come in as rows of V values.
  *
@@ -64,9 +68,13 @@ enum {
                                    weight); accepted iff its residual mass is > 0 */
     RSD_ST_DRAFT_EXHAUSTED = 16, /* the draft had no mass left after a removal (in fp32: nothing above 2^-126 of the
                                     row's largest weight); later siblings were ignored */
-    RSD_ST_TIMEOUT = 32         /* an on-chip copy of a row did not complete within about a second (a hardware or
+    RSD_ST_TIMEOUT = 32,        /* an on-chip copy of a row did not complete within about a second (a hardware or
                                    driver fault, never a property of the data): the walk of this sequence was
                                    abandoned, accepted_len counts what was accepted before, last_token is -1 */
+    RSD_ST_ZERO_TARGET_PROB = 64, /* scoring: a token with draft mass has target probability 0, so that KL(p||q) is infinite
+                                   (RSD_ST_ZERO_DRAFT_PROB: the other way round, KL(q||p) is infinite) */
+    RSD_ST_EMPTY_ROW = 128,     /* scoring: a row without any entry (all -inf, NaN or +inf) */
+    RSD_ST_BAD_INDEX = 256      /* scoring: a token >= V or a row index >= the rows there are; it counts as absent */
 };
 
 /* stop_reason[b] of the verification walk */
@@ -295,6 +303,76 @@ int rsd_resample_residual(const rsd_rows* draft_row, const rsd_rows* target_row,
                           const int32_t* rejected, int max_k, const int32_t* rng_node, uint64_t seed, uint32_t step,
                           uint32_t seq_base, int32_t* out_token, float* out_residual, int32_t* status,
                           rsd_stream_t stream);
+
+/*
+ * Scoring of rows: log-probabilities of given tokens, the entropy and the likeliest tokens, p = softmax(row / temperature).
+ * Rows given as log-probabilities are renormalised like logits.  -inf entries have probability 0; NaN and +inf entries count as
+ * -inf (RSD_ST_NAN_INPUT).  A row without entries (RSD_ST_EMPTY_ROW) has log-probabilities of -inf, entropy 0 and no likeliest tokens.
+ * A row's outputs have the same bits in every launch: whatever the rows beside it and the address that it starts at.
+ *   rows         [B][num_rows][V]
+ *   row_index    optional [B][R] int32: slot r of a sequence is row row_index[b][r] (< 0: an empty slot); NULL: slot r is row r,
+ *                and R may not exceed num_rows
+ *   token        [B][R][T] int32 (T <= RSD_MAX_K; T = 0: NULL); < 0: absent
+ *   out_logprob  [B][R][T] fp32: ln p(token); 0 where the token is absent or the slot empty (so that sums over slots stay right), -inf where the
+ *                token has probability 0
+ *   out_entropy  optional [B][R] fp32: -sum p ln p (0 for an empty slot)
+ *   out_top_token, out_top_logprob   [B][R][K] int32 / fp32, K <= RSD_MAX_K (K = 0: NULL): the K largest entries in decreasing order,
+ *                equal values to the smaller token, and their ln p; -1 and -inf beyond the row's entries (RSD_ST_FEWER_THAN_K)
+ *   status       [B]: OR over the slots of a sequence
+ * Outputs may not overlap the inputs or each other.
+ */
+int rsd_token_logprobs(const rsd_rows* rows, int B, int R, int V, int num_rows, const int32_t* row_index, const int32_t* token, int T,
+                       int K, float* out_logprob, float* out_entropy, int32_t* out_top_token, float* out_top_logprob,
+                       int32_t* status, rsd_stream_t stream);
+
+/*
+ * rsd_token_logprobs for what a verification emitted (accepted_len, accepted_node, accepted_token [B][L], last_token as rsd_verify_tree
+ * wrote them): slot r <= accepted_len[b] of a sequence is the target row that its r-th emitted token was tested on or drawn from
+ * (the root's, then those of the accepted nodes), with that token; the L + 1 slots beyond are empty.  Only visited rows are read.
+ *   target       rows of all nodes [B][num_nodes][V], with the temperature of the verification
+ *   out_token    optional [B][L + 1] int32: the emitted tokens in order, -1 beyond
+ *   out_logprob [B][L + 1], out_entropy, out_top_token, out_top_logprob, status   as above
+ * accepted_len[b] outside [0, L] leaves all slots of the sequence empty.
+ */
+int rsd_emitted_logprobs(const rsd_rows* target, int B, int num_nodes, int V, int L, const int32_t* accepted_len,
+                         const int32_t* accepted_node, const int32_t* accepted_token, const int32_t* last_token, int K,
+                         int32_t* out_token, float* out_logprob, float* out_entropy, int32_t* out_top_token,
+                         float* out_top_logprob, int32_t* status, rsd_stream_t stream);
+
+/*
+ * Gradient of  sum_t grad_logprob[b][r][t] ln p(token[b][r][t]) + grad_entropy[b][r] H(b, r)  with respect to the stored values v of
+ * the rows (the division by the temperature T included):
+ *   ( sum_{t: token_t = x} g_t - p_x (sum_t g_t + h (ln p_x + H)) ) / T
+ * The normalisers are taken from the row again, so that nothing has to be kept from the forward call.  A token given twice counts twice,
+ * an absent one not at all; entries without probability get what the formula gives at p_x = 0; a row without entries gets 0 throughout.
+ *   rows [B][R][V];  token [B][R][T], 1 <= T <= RSD_MAX_K;  grad_logprob [B][R][T], grad_entropy optional [B][R], fp32
+ *   grad_rows    [B][R][V] dense, the rows' element type, rounded once; may not overlap the rows
+ */
+int rsd_token_logprobs_backward(const rsd_rows* rows, int B, int R, int V, const int32_t* token, int T, const float* grad_logprob,
+                                const float* grad_entropy, void* grad_rows, int32_t* status, rsd_stream_t stream);
+
+/*
+ * How far draft rows p are from target rows q (p, q = softmax of the rows over their temperatures):
+ *   out_kl          KL(q||p) = sum q (ln q - ln p): what a drafter is trained on
+ *   out_reverse_kl  KL(p||q)
+ *   out_overlap     sum min(p, q): the probability that a verification accepts one draft (Section 2), 1 - total variation distance
+ * each optional [B][R] fp32, at least one of them.  Row r of a sequence's draft is paired with row r of its target (flat node r of a
+ * tree), so that the target may have more rows.  Terms with weight 0 are 0; a weight below 2^-126 of its row's largest counts as 0.  A token
+ * with mass in one row only makes the divergence from that row infinite (RSD_ST_ZERO_DRAFT_PROB, RSD_ST_ZERO_TARGET_PROB).  NaN
+ * and +inf entries count as -inf (RSD_ST_NAN_INPUT); where either row has no entry all three are 0 (RSD_ST_EMPTY_ROW).
+ * draft and target must have the same dtype.  The outputs have the same bits in every launch.
+ */
+int rsd_row_divergence(const rsd_rows* draft, const rsd_rows* target, int B, int R, int V, float* out_kl, float* out_reverse_kl,
+                       float* out_overlap, int32_t* status, rsd_stream_t stream);
+
+/*
+ * Gradient of  grad_kl[b][r] KL(q||p) + grad_reverse_kl[b][r] KL(p||q)  with respect to the stored values of the draft rows:
+ *   ( g (p_x - q_x) + h p_x (ln p_x - ln q_x - KL(p||q)) ) / T_draft
+ * (either may be NULL, not both).  A row whose KL(p||q) is infinite gets no gradient of it; a pair of rows of which one has no entry gets 0.
+ *   grad_draft   [B][R][V] dense, the rows' element type, rounded once; may not overlap the rows
+ */
+int rsd_row_divergence_backward(const rsd_rows* draft, const rsd_rows* target, int B, int R, int V, const float* grad_kl,
+                                const float* grad_reverse_kl, void* grad_draft, int32_t* status, rsd_stream_t stream);
 
 #ifdef __cplusplus
 }

@@ -6,8 +6,11 @@
 #include <dlfcn.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 
+#include <climits>
+#include <initializer_list>
 #include <vector>
 
 #include "../../include/rsd.h"
@@ -25,6 +28,11 @@ decltype(&rsd_sbs_draft_tree) p_sbs_draft_tree;
 decltype(&rsd_verify_tree) p_verify_tree;
 decltype(&rsd_verify_tree_rule) p_verify_tree_rule;
 decltype(&rsd_resample_residual) p_resample;
+decltype(&rsd_token_logprobs) p_token_logprobs;
+decltype(&rsd_emitted_logprobs) p_emitted_logprobs;
+decltype(&rsd_token_logprobs_backward) p_token_logprobs_backward;
+decltype(&rsd_row_divergence) p_row_divergence;
+decltype(&rsd_row_divergence_backward) p_row_divergence_backward;
 
 struct Failed {};   // a Python error is set
 
@@ -282,6 +290,147 @@ PyObject* resample_residual(PyObject* const* a) {
     return call([&] { return p_resample(&d, &t, B, V, rejected, max_k, node, seed, step, seq, token, residual, status, s); });
 }
 
+// ---- scoring of rows: every tensor is checked against the rows' device, its type and its shape --------------------------------------------
+// The data of a contiguous tensor of this type and shape on the rows' device (None: null where it may be left out).
+void* data_of(PyObject* o, const char* name, at::ScalarType type, const at::Tensor& rows, std::initializer_list<int64_t> shape, bool optional = false) {
+    if (o == Py_None && optional) return nullptr;
+    const at::Tensor& t = tensor(o);
+    if (t.device() != rows.device()) {
+        PyErr_Format(g_error, "%s must live on the rows' device", name);
+        throw Failed();
+    }
+    if (t.scalar_type() != type || !t.is_contiguous()) {
+        PyErr_Format(g_error, "%s must be contiguous %s", name, type == at::kInt ? "int32" : type == at::kFloat ? "float32" : "and of the rows' dtype");
+        throw Failed();
+    }
+    if (t.sizes() != at::IntArrayRef(shape)) {
+        PyErr_Format(g_error, "%s has the wrong shape", name);
+        throw Failed();
+    }
+    return t.data_ptr();
+}
+struct Batch {
+    int B, R, V;
+};
+Batch batch_of(const at::Tensor& t) {
+    want_dims(t, 3);
+    for (int i = 0; i < 3; ++i)
+        if (t.size(i) > INT_MAX) fail("rows: too many of them");
+    return {(int)t.size(0), (int)t.size(1), (int)t.size(2)};
+}
+
+// rows, temperature, row_index, token, K, logprob, entropy, top_token, top_logprob, status
+PyObject* token_logprobs(PyObject* const* a) {
+    const at::Tensor& t = tensor(a[0]);
+    const Batch n = batch_of(t);
+    const rsd_rows r = rows_of(t, false, real(a[1]));
+    const int K = (int)integer(a[4]);
+    int64_t R = n.R, T = 0;
+    const bool flat = a[3] != Py_None && tensor(a[3]).dim() == 2;    // one token a slot, without a dimension of its own
+    if (a[2] != Py_None) {
+        want_dims(tensor(a[2]), 2);
+        R = tensor(a[2]).size(1);
+    }
+    if (a[3] != Py_None) {
+        if (!flat) want_dims(tensor(a[3]), 3);
+        T = flat ? 1 : tensor(a[3]).size(2);
+        if (a[2] == Py_None) R = tensor(a[3]).size(1);
+    }
+    if (R > INT_MAX || T > INT_MAX) fail("token: too many of them");
+    const int32_t* index = (const int32_t*)data_of(a[2], "row_index", at::kInt, t, {n.B, R}, true);
+    const int32_t* token = (const int32_t*)(flat ? data_of(a[3], "token", at::kInt, t, {n.B, R}) : data_of(a[3], "token", at::kInt, t, {n.B, R, T}, true));
+    float* logprob = (float*)(flat ? data_of(a[5], "logprob", at::kFloat, t, {n.B, R}) : data_of(a[5], "logprob", at::kFloat, t, {n.B, R, T}, T == 0));
+    float* entropy = (float*)data_of(a[6], "entropy", at::kFloat, t, {n.B, R}, true);
+    int32_t* top_token = (int32_t*)data_of(a[7], "top_token", at::kInt, t, {n.B, R, K}, K == 0);
+    float* top_logprob = (float*)data_of(a[8], "top_logprob", at::kFloat, t, {n.B, R, K}, K == 0);
+    int32_t* status = (int32_t*)data_of(a[9], "status", at::kInt, t, {n.B});
+    if (n.B == 0) Py_RETURN_NONE;
+    const c10::cuda::CUDAGuard device(t.device());
+    const rsd_stream_t s = stream();
+    return call([&] { return p_token_logprobs(&r, n.B, (int)R, n.V, n.R, index, token, (int)T, K, logprob, entropy, top_token, top_logprob, status, s); });
+}
+
+// target, temperature, accepted_len, accepted_node, accepted_token, last_token, K, token, logprob, entropy, top_token, top_logprob, status
+PyObject* emitted_logprobs(PyObject* const* a) {
+    const at::Tensor& t = tensor(a[0]);
+    const Batch n = batch_of(t);
+    const rsd_rows r = rows_of(t, false, real(a[1]));
+    want_dims(tensor(a[3]), 2);
+    const int64_t L = tensor(a[3]).size(1);
+    if (L >= RSD_MAX_TREE_NODES) fail("accepted_node: too many levels");
+    const int K = (int)integer(a[6]);
+    const int32_t *len = (const int32_t*)data_of(a[2], "accepted_len", at::kInt, t, {n.B}), *node = (const int32_t*)data_of(a[3], "accepted_node", at::kInt, t, {n.B, L}),
+                  *tok = (const int32_t*)data_of(a[4], "accepted_token", at::kInt, t, {n.B, L}), *last = (const int32_t*)data_of(a[5], "last_token", at::kInt, t, {n.B});
+    int32_t* token = (int32_t*)data_of(a[7], "token", at::kInt, t, {n.B, L + 1}, true);
+    float *logprob = (float*)data_of(a[8], "logprob", at::kFloat, t, {n.B, L + 1}), *entropy = (float*)data_of(a[9], "entropy", at::kFloat, t, {n.B, L + 1}, true);
+    int32_t* top_token = (int32_t*)data_of(a[10], "top_token", at::kInt, t, {n.B, L + 1, K}, K == 0);
+    float* top_logprob = (float*)data_of(a[11], "top_logprob", at::kFloat, t, {n.B, L + 1, K}, K == 0);
+    int32_t* status = (int32_t*)data_of(a[12], "status", at::kInt, t, {n.B});
+    if (n.B == 0) Py_RETURN_NONE;
+    const c10::cuda::CUDAGuard device(t.device());
+    const rsd_stream_t s = stream();
+    return call([&] {
+        return p_emitted_logprobs(&r, n.B, n.R, n.V, (int)L, len, node, tok, last, K, token, logprob, entropy, top_token, top_logprob, status, s);
+    });
+}
+
+// rows, temperature, token, grad_logprob, grad_entropy, grad_rows, status
+PyObject* token_logprobs_backward(PyObject* const* a) {
+    const at::Tensor &t = tensor(a[0]), &tok = tensor(a[2]);
+    const Batch n = batch_of(t);
+    const rsd_rows r = rows_of(t, false, real(a[1]));
+    const bool flat = tok.dim() == 2;
+    if (!flat) want_dims(tok, 3);
+    const int64_t T = flat ? 1 : tok.size(2);
+    if (T > INT_MAX) fail("token: too many of them");
+    const int32_t* token = (const int32_t*)(flat ? data_of(a[2], "token", at::kInt, t, {n.B, n.R}) : data_of(a[2], "token", at::kInt, t, {n.B, n.R, T}));
+    const float* g = (const float*)(flat ? data_of(a[3], "grad_logprob", at::kFloat, t, {n.B, n.R}) : data_of(a[3], "grad_logprob", at::kFloat, t, {n.B, n.R, T}));
+    const float* h = (const float*)data_of(a[4], "grad_entropy", at::kFloat, t, {n.B, n.R}, true);
+    void* grad = data_of(a[5], "grad_rows", t.scalar_type(), t, {n.B, n.R, n.V});
+    int32_t* status = (int32_t*)data_of(a[6], "status", at::kInt, t, {n.B});
+    if (n.B == 0) Py_RETURN_NONE;
+    const c10::cuda::CUDAGuard device(t.device());
+    const rsd_stream_t s = stream();
+    return call([&] { return p_token_logprobs_backward(&r, n.B, n.R, n.V, token, (int)T, g, h, grad, status, s); });
+}
+
+// The target rows that belong to a batch of draft rows: as many sequences, at least as many rows, as long.
+void check_pair(const at::Tensor& target, const at::Tensor& draft, const Batch& n) {
+    const Batch m = batch_of(target);
+    if (target.device() != draft.device()) fail("draft and target rows must live on one device");
+    if (m.B != n.B || m.R < n.R || m.V != n.V) fail("target must hold the draft's sequences, at least as many rows of each, and rows as long");
+}
+
+// draft, draft temperature, target, target temperature, kl, reverse_kl, overlap, status
+PyObject* row_divergence(PyObject* const* a) {
+    const at::Tensor &d = tensor(a[0]), &t = tensor(a[2]);
+    const Batch n = batch_of(d);
+    check_pair(t, d, n);
+    const rsd_rows dr = rows_of(d, false, real(a[1])), tr = rows_of(t, false, real(a[3]));
+    float *kl = (float*)data_of(a[4], "kl", at::kFloat, d, {n.B, n.R}, true), *reverse = (float*)data_of(a[5], "reverse_kl", at::kFloat, d, {n.B, n.R}, true),
+          *overlap = (float*)data_of(a[6], "overlap", at::kFloat, d, {n.B, n.R}, true);
+    int32_t* status = (int32_t*)data_of(a[7], "status", at::kInt, d, {n.B});
+    if (n.B == 0) Py_RETURN_NONE;
+    const c10::cuda::CUDAGuard device(d.device());
+    const rsd_stream_t s = stream();
+    return call([&] { return p_row_divergence(&dr, &tr, n.B, n.R, n.V, kl, reverse, overlap, status, s); });
+}
+
+// draft, draft temperature, target, target temperature, grad_kl, grad_reverse_kl, grad_draft, status
+PyObject* row_divergence_backward(PyObject* const* a) {
+    const at::Tensor &d = tensor(a[0]), &t = tensor(a[2]);
+    const Batch n = batch_of(d);
+    check_pair(t, d, n);
+    const rsd_rows dr = rows_of(d, false, real(a[1])), tr = rows_of(t, false, real(a[3]));
+    const float *g = (const float*)data_of(a[4], "grad_kl", at::kFloat, d, {n.B, n.R}, true), *h = (const float*)data_of(a[5], "grad_reverse_kl", at::kFloat, d, {n.B, n.R}, true);
+    void* grad = data_of(a[6], "grad_draft", d.scalar_type(), d, {n.B, n.R, n.V});
+    int32_t* status = (int32_t*)data_of(a[7], "status", at::kInt, d, {n.B});
+    if (n.B == 0) Py_RETURN_NONE;
+    const c10::cuda::CUDAGuard device(d.device());
+    const rsd_stream_t s = stream();
+    return call([&] { return p_row_divergence_backward(&dr, &tr, n.B, n.R, n.V, g, h, grad, status, s); });
+}
+
 // bind(path of librsd, exception class)
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const char* path = n == 2 ? PyUnicode_AsUTF8(a[0]) : nullptr;
@@ -313,6 +462,11 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
     find(p_verify_tree, "rsd_verify_tree");
     find(p_verify_tree_rule, "rsd_verify_tree_rule");
     find(p_resample, "rsd_resample_residual");
+    find(p_token_logprobs, "rsd_token_logprobs");
+    find(p_emitted_logprobs, "rsd_emitted_logprobs");
+    find(p_token_logprobs_backward, "rsd_token_logprobs_backward");
+    find(p_row_divergence, "rsd_row_divergence");
+    find(p_row_divergence_backward, "rsd_row_divergence_backward");
     if (!all) {
         PyErr_Format(PyExc_OSError, "%s lacks an entry point", path);
         return nullptr;
@@ -336,6 +490,11 @@ PyMethodDef methods[] = {
     RSD_ENTRY(sbs_draft_tree, 15),
     RSD_ENTRY(verify_tree, 21),
     RSD_ENTRY(resample_residual, 12),
+    RSD_ENTRY(token_logprobs, 10),
+    RSD_ENTRY(emitted_logprobs, 13),
+    RSD_ENTRY(token_logprobs_backward, 7),
+    RSD_ENTRY(row_divergence, 8),
+    RSD_ENTRY(row_divergence_backward, 8),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_rsdbind", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -1,0 +1,224 @@
+// Rows dealt out in tiles to warps: what the kernels that score rows share.
+//
+// A tile is KW words of 16 bytes per lane: word k of lane l of tile t holds the entries that start at ((t KW + k) 32 + l) E of the row, E entries a word.
+// Everything that is summed is summed per tile, relative to the tile's own maximum, by one warp in a fixed order, and the tiles' sums
+// are joined in the order of the tiles.  So a row gives the same bits whatever the number of warps or blocks that share it, the rows beside it
+// and the address that it starts at.
+#pragma once
+#include "rsd_device.cuh"
+#include "rsd_scan.cuh"   // ex2_approx, packed arithmetic
+
+namespace rsd {
+namespace tiles {
+
+// A row as 16-byte granules from the one that holds its first entry (an allocation holds whole granules, so that what lies around the row in its first and last
+// granule may be read; it is masked).
+struct View {
+    const char* base;     // 16-byte aligned
+    int first;            // bytes from base to the first entry
+    int last;             // index of the granule that holds the last entry
+};
+template <typename T>
+__device__ __forceinline__ View view_of(const void* row, int V) {
+    const int first = (int)((uintptr_t)row & 15u);
+    return {(const char*)row - first, first, (first + V * (int)sizeof(T) - 1) >> 4};
+}
+
+// bytes shift .. shift + 15 of two adjacent granules
+__device__ __forceinline__ uint4 shifted(const uint4& a, const uint4& b, int shift) {
+    const bool one = shift & 4, two = shift & 8;
+    const uint32_t x0 = one ? a.y : a.x, x1 = one ? a.z : a.y, x2 = one ? a.w : a.z, x3 = one ? b.x : a.w, x4 = one ? b.y : b.x, x5 = one ? b.z : b.y, x6 = one ? b.w : b.z;
+    const uint32_t y0 = two ? x2 : x0, y1 = two ? x3 : x1, y2 = two ? x4 : x2, y3 = two ? x5 : x3, y4 = two ? x6 : x4;
+    const int bits = (shift & 3) * 8;
+    return make_uint4(__funnelshift_r(y0, y1, bits), __funnelshift_r(y1, y2, bits), __funnelshift_r(y2, y3, bits), __funnelshift_r(y3, y4, bits));
+}
+
+template <typename T>
+struct Packed16;   // one word as entries
+
+template <>
+struct Packed16<float> {
+    static constexpr int kEntries = 4;
+    static constexpr uint32_t kMasked = 0xFF800000u;
+    __device__ static __forceinline__ float get(const uint4& w, int i) { return __uint_as_float(i == 0 ? w.x : i == 1 ? w.y : i == 2 ? w.z : w.w); }
+    // entries outside [from, to) become -inf
+    __device__ static __forceinline__ void keep(uint4& w, int from, int to) {
+        if (from > 0 || to < 1) w.x = kMasked;
+        if (from > 1 || to < 2) w.y = kMasked;
+        if (from > 2 || to < 3) w.z = kMasked;
+        if (from > 3 || to < 4) w.w = kMasked;
+    }
+    __device__ static __forceinline__ uint32_t clean_entry(uint32_t u, bool& bad) {   // NaN and +inf are no entries
+        const bool b = !(__uint_as_float(u) < __builtin_huge_valf());
+        bad |= b;
+        return b ? kMasked : u;
+    }
+    __device__ static __forceinline__ void clean(uint4& w, bool& bad) {
+        w.x = clean_entry(w.x, bad), w.y = clean_entry(w.y, bad), w.z = clean_entry(w.z, bad), w.w = clean_entry(w.w, bad);
+    }
+    __device__ static __forceinline__ uint4 masked() { return make_uint4(kMasked, kMasked, kMasked, kMasked); }
+    template <int KW>
+    __device__ static __forceinline__ void bounds(const uint4 (&w)[KW], float& mx, float& mn) {   // mx: NaN if there is one
+        float a = __uint_as_float(w[0].x), b = a;
+#pragma unroll
+        for (int k = 0; k < KW; ++k) {
+            const float p = max_nan(__uint_as_float(w[k].x), __uint_as_float(w[k].y)), q = max_nan(__uint_as_float(w[k].z), __uint_as_float(w[k].w));
+            a = max_nan(a, max_nan(p, q));
+            const float r = fminf(__uint_as_float(w[k].x), __uint_as_float(w[k].y)), s = fminf(__uint_as_float(w[k].z), __uint_as_float(w[k].w));
+            b = fminf(b, fminf(r, s));
+        }
+        mx = a, mn = b;
+    }
+    // f(pair of entries) for the pairs of a word
+    template <typename F>
+    __device__ static __forceinline__ void pairs(const uint4& w, F f) {
+        f(f32x2(__uint_as_float(w.x), __uint_as_float(w.y)));
+        f(f32x2(__uint_as_float(w.z), __uint_as_float(w.w)));
+    }
+    // a word from its entries
+    template <typename F>
+    __device__ static __forceinline__ uint4 make(F f) {
+        float a[4];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) split_f32x2(f(i), a[2 * i], a[2 * i + 1]);
+        return make_uint4(__float_as_uint(a[0]), __float_as_uint(a[1]), __float_as_uint(a[2]), __float_as_uint(a[3]));
+    }
+    __device__ static __forceinline__ unsigned long long pair(const uint4& w, int i) {
+        return i == 0 ? f32x2(__uint_as_float(w.x), __uint_as_float(w.y)) : f32x2(__uint_as_float(w.z), __uint_as_float(w.w));
+    }
+    __device__ static __forceinline__ void store(void* row, int x, float v) { ((float*)row)[x] = v; }
+};
+
+template <>
+struct Packed16<__nv_bfloat16> {
+    static constexpr int kEntries = 8;
+    static constexpr uint32_t kMasked = 0xFF80FF80u;
+    __device__ static __forceinline__ float get(const uint4& w, int i) {
+        const uint32_t u = (i >> 1) == 0 ? w.x : (i >> 1) == 1 ? w.y : (i >> 1) == 2 ? w.z : w.w;
+        return __uint_as_float((i & 1) ? (u & 0xFFFF0000u) : (u << 16));
+    }
+    __device__ static __forceinline__ uint32_t keep_entry(uint32_t u, int i, int from, int to) {
+        if (from > i || to <= i) u = (u & 0xFFFF0000u) | 0xFF80u;
+        if (from > i + 1 || to <= i + 1) u = (u & 0xFFFFu) | 0xFF800000u;
+        return u;
+    }
+    __device__ static __forceinline__ void keep(uint4& w, int from, int to) {
+        w.x = keep_entry(w.x, 0, from, to), w.y = keep_entry(w.y, 2, from, to), w.z = keep_entry(w.z, 4, from, to), w.w = keep_entry(w.w, 6, from, to);
+    }
+    __device__ static __forceinline__ uint32_t clean_entry(uint32_t u, bool& bad) {
+        const bool lo = !(__uint_as_float(u << 16) < __builtin_huge_valf()), hi = !(__uint_as_float(u & 0xFFFF0000u) < __builtin_huge_valf());
+        bad |= lo | hi;
+        if (lo) u = (u & 0xFFFF0000u) | 0xFF80u;
+        if (hi) u = (u & 0xFFFFu) | 0xFF800000u;
+        return u;
+    }
+    __device__ static __forceinline__ void clean(uint4& w, bool& bad) {
+        w.x = clean_entry(w.x, bad), w.y = clean_entry(w.y, bad), w.z = clean_entry(w.z, bad), w.w = clean_entry(w.w, bad);
+    }
+    __device__ static __forceinline__ uint4 masked() { return make_uint4(kMasked, kMasked, kMasked, kMasked); }
+    __device__ static __forceinline__ uint32_t min2(uint32_t a, uint32_t b) {
+        uint32_t r;
+        asm("min.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+        return r;
+    }
+    template <int KW>
+    __device__ static __forceinline__ void bounds(const uint4 (&w)[KW], float& mx, float& mn) {
+        uint32_t a = w[0].x, b = w[0].x;
+#pragma unroll
+        for (int k = 0; k < KW; ++k) {
+            a = bf162_max_nan(a, bf162_max_nan(bf162_max_nan(w[k].x, w[k].y), bf162_max_nan(w[k].z, w[k].w)));
+            b = min2(b, min2(min2(w[k].x, w[k].y), min2(w[k].z, w[k].w)));
+        }
+        mx = max_nan(__uint_as_float(a << 16), __uint_as_float(a & 0xFFFF0000u));
+        mn = fminf(__uint_as_float(b << 16), __uint_as_float(b & 0xFFFF0000u));
+    }
+    __device__ static __forceinline__ unsigned long long unpack(uint32_t u) { return f32x2(__uint_as_float(u << 16), __uint_as_float(u & 0xFFFF0000u)); }
+    template <typename F>
+    __device__ static __forceinline__ void pairs(const uint4& w, F f) {
+        f(unpack(w.x)), f(unpack(w.y)), f(unpack(w.z)), f(unpack(w.w));
+    }
+    __device__ static __forceinline__ uint32_t pack(unsigned long long v) {   // rounded to nearest even, once
+        float lo, hi;
+        split_f32x2(v, lo, hi);
+        uint32_t r;
+        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+        return r;
+    }
+    template <typename F>
+    __device__ static __forceinline__ uint4 make(F f) { return make_uint4(pack(f(0)), pack(f(1)), pack(f(2)), pack(f(3))); }
+    __device__ static __forceinline__ unsigned long long pair(const uint4& w, int i) { return unpack(i == 0 ? w.x : i == 1 ? w.y : i == 2 ? w.z : w.w); }
+    __device__ static __forceinline__ void store(void* row, int x, float v) { ((__nv_bfloat16*)row)[x] = __float2bfloat16_rn(v); }
+};
+
+__device__ __forceinline__ unsigned long long mul_f32x2(unsigned long long a, unsigned long long b) {
+    unsigned long long r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ unsigned long long both(float v) { return f32x2(v, v); }
+
+template <typename T>
+__host__ __device__ constexpr int tile_entries(int KW) { return KW * 32 * (16 / (int)sizeof(T)); }
+template <typename T>
+__host__ __device__ constexpr int tiles_of(int V, int KW) { return (V + tile_entries<T>(KW) - 1) / tile_entries<T>(KW); }
+
+// The word that starts at entry x0 (which may lie before or behind the row), entries outside the row as -inf.
+// ALIGNED: x0 lies on a 16-byte boundary.
+template <typename T, bool ALIGNED>
+__device__ __forceinline__ uint4 load_word(const View& v, int x0, int V) {
+    constexpr int E = Packed16<T>::kEntries;
+    if (x0 >= V || x0 + E <= 0) return Packed16<T>::masked();
+    const int at = v.first + x0 * (int)sizeof(T), g = at >> 4, shift = at & 15;
+    uint4 w = make_uint4(0, 0, 0, 0);
+    if (ALIGNED || shift == 0) {
+        w = ld_stream(v.base + (int64_t)g * 16);
+    } else {
+        uint4 b = w;
+        if (g >= 0) w = ld_shared_word(v.base + (int64_t)g * 16);
+        if (g < v.last) b = ld_shared_word(v.base + (int64_t)(g + 1) * 16);
+        w = shifted(w, b, shift);
+    }
+    if (x0 < 0 || x0 + E > V) Packed16<T>::keep(w, -x0, V - x0);
+    return w;
+}
+
+template <typename T, bool ALIGNED, int KW>
+__device__ __forceinline__ void load_tile(uint4 (&w)[KW], const View& v, int t, int lane, int V) {
+#pragma unroll
+    for (int k = 0; k < KW; ++k) w[k] = load_word<T, ALIGNED>(v, ((t * KW + k) * 32 + lane) * Packed16<T>::kEntries, V);
+}
+
+__device__ __forceinline__ float warp_max_nan(float v) {   // NaN if any lane has one
+    float r;
+    asm volatile("redux.sync.max.NaN.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+    return r;
+}
+
+// Two sums over the warp at once, in an order of their own: the first in lanes 0 to 15, the second in the others.
+__device__ __forceinline__ float warp_sum_two(float a, float b, int lane) {
+    const bool high = lane & 16;
+    float mine = high ? b : a;
+    const float other = high ? a : b;
+    mine += __shfl_xor_sync(0xFFFFFFFFu, other, 16);
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) mine += __shfl_xor_sync(0xFFFFFFFFu, mine, o);
+    return mine;
+}
+// Four sums: lanes 0 to 7, 8 to 15, 16 to 23, 24 to 31.
+__device__ __forceinline__ float warp_sum_four(float a, float b, float c, float d, int lane) {
+    const bool high = lane & 16, second = lane & 8;
+    float p = high ? c : a, q = high ? d : b;
+    p += __shfl_xor_sync(0xFFFFFFFFu, high ? a : c, 16);
+    q += __shfl_xor_sync(0xFFFFFFFFu, high ? b : d, 16);
+    float mine = second ? q : p;
+    mine += __shfl_xor_sync(0xFFFFFFFFu, second ? p : q, 8);
+#pragma unroll
+    for (int o = 4; o > 0; o >>= 1) mine += __shfl_xor_sync(0xFFFFFFFFu, mine, o);
+    return mine;
+}
+
+// Exponents below this give weights of 0 and may be replaced by it: 0 times it is 0, where 0 times -inf is not a number.
+constexpr float kFarBelow = -1e30f;
+
+}  // namespace tiles
+}  // namespace rsd

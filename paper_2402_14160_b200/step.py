@@ -3,18 +3,33 @@
 These classes only own buffers and issue the C-ABI calls in order (Algorithm 2 for constant branching factors,
 Algorithm 7 for Stochastic Beam Search, with the language-model calls replaced by rows that already sit in device
 memory).  The drafting calls write the tree's token/parent arrays in place, so no tensor work happens between the
-library's kernels.
+library's kernels.  With `logprobs=K` a step ends with the log-probabilities of the tokens that it emitted and K alternatives each
+(`emitted_out`), as a server returns them.
 """
 from __future__ import annotations
 
-from typing import Sequence
+from typing import Optional, Sequence
 
 import torch
 
 from . import api
 
 
-class RsdCStep:
+class _Step:
+    """What both kinds of step do behind the walk."""
+
+    emitted_out = None
+
+    def score_emitted(self, target: torch.Tensor, top_k: int = 0):
+        """rsd_emitted_logprobs of the last walk over these target rows."""
+        out = self.emitted_out
+        if out is not None and (0 if out["top_token"] is None else out["top_token"].shape[2]) != top_k:
+            out = None
+        self.emitted_out = api.rsd_emitted_logprobs(target, self.verify_out, top_k=top_k, out=out)
+        return self.emitted_out
+
+
+class RsdCStep(_Step):
     """RSD with constant branching factors b = (b_0, ..., b_{L-1}) for a batch of B sequences."""
 
     def __init__(self, B: int, V: int, branching: Sequence[int], device="cuda"):
@@ -45,16 +60,18 @@ class RsdCStep:
         self.verify_out = None
         self.kernel_launches = 2  # one scan, one walk
 
-    def run(self, draft: torch.Tensor, target: torch.Tensor, seed: int, step: int, seq_base: int = 0):
+    def run(self, draft: torch.Tensor, target: torch.Tensor, seed: int, step: int, seq_base: int = 0, logprobs: Optional[int] = None):
         api.rsd_gumbel_topk_draft(draft, self.k_per_row, self.rng_node, seed, step, seq_base=seq_base,
                                   max_k=self.max_k, child_base=self.child_base, node_token=self.token,
                                   out=self.draft_out)
         self.verify_out = api.rsd_verify_tree(draft, target, self.parent, self.token, self.L, seed, step,
                                               seq_base=seq_base, out=self.verify_out)
+        if logprobs is not None:
+            self.score_emitted(target, logprobs)
         return self.verify_out
 
 
-class RsdSStep:
+class RsdSStep(_Step):
     """RSD with Stochastic Beam Search of width W and depth L for a batch of B sequences.
 
     rows_ready=True: the draft rows of every level exist before drafting starts (rows attached to tree slots), so the
@@ -89,12 +106,14 @@ class RsdSStep:
                                       is_logprob=self.is_logprob, seq_base=seq_base, workspace=self.workspace,
                                       out=self.tree_out)
 
-    def run(self, draft: torch.Tensor, target: torch.Tensor, seed: int, step: int, seq_base: int = 0):
+    def run(self, draft: torch.Tensor, target: torch.Tensor, seed: int, step: int, seq_base: int = 0, logprobs: Optional[int] = None):
         W = self.W
         if self.rows_ready:
             self.draft_tree(draft, seed, step, seq_base)
             self.verify_out = api.rsd_verify_tree(draft, target, self.parent, self.token, self.L, seed, step,
                                                   seq_base=seq_base, out=self.verify_out)
+            if logprobs is not None:
+                self.score_emitted(target, logprobs)
             return self.verify_out
         for l in range(self.L):
             first = 0 if l == 0 else 1 + (l - 1) * W
@@ -108,6 +127,8 @@ class RsdSStep:
                              seq_base=seq_base, workspace=self.workspace, out=out, parent_base=first)
         self.verify_out = api.rsd_verify_tree(draft, target, self.parent, self.token, self.L, seed, step,
                                               seq_base=seq_base, out=self.verify_out)
+        if logprobs is not None:
+            self.score_emitted(target, logprobs)
         return self.verify_out
 
 
