@@ -20,7 +20,7 @@
  *   - The return value reports argument and launch errors only (RSD_OK = 0); rsd_last_error() gives a message for
  *     the calling thread.  Data-dependent trouble (NaN logits, rows with fewer than k finite entries, an empty
  *     residual) never traps: it sets bits in the per-sequence `status` output and follows the documented fallback.
- *     Each call overwrites status[0..B).
+ *     Each call overwrites status[0..B) (the scoring calls, whose rows are asked about one by one: status[0..B R)).
  *   - Rows: element (b, r, x) of a batch of rows sits at data + b*seq_stride + r*row_stride + x (strides in
  *     elements).  fp32 or bf16 storage; all arithmetic is fp32 or wider.  The vectorised path needs the base
  *     pointer and both strides to be multiples of 16 bytes; anything else takes a slower scalar path with the same
@@ -318,7 +318,7 @@ int rsd_resample_residual(const rsd_rows* draft_row, const rsd_rows* target_row,
  *   out_entropy  optional [B][R] fp32: -sum p ln p (0 for an empty slot)
  *   out_top_token, out_top_logprob   [B][R][K] int32 / fp32, K <= RSD_MAX_K (K = 0: NULL): the K largest entries in decreasing order,
  *                equal values to the smaller token, and their ln p; -1 and -inf beyond the row's entries (RSD_ST_FEWER_THAN_K)
- *   status       [B]: OR over the slots of a sequence
+ *   status       [B][R], of each slot
  * Outputs may not overlap the inputs or each other.
  */
 int rsd_token_logprobs(const rsd_rows* rows, int B, int R, int V, int num_rows, const int32_t* row_index, const int32_t* token, int T,
@@ -331,7 +331,7 @@ int rsd_token_logprobs(const rsd_rows* rows, int B, int R, int V, int num_rows, 
  * (the root's, then those of the accepted nodes), with that token; the L + 1 slots beyond are empty.  Only visited rows are read.
  *   target       rows of all nodes [B][num_nodes][V], with the temperature of the verification
  *   out_token    optional [B][L + 1] int32: the emitted tokens in order, -1 beyond
- *   out_logprob [B][L + 1], out_entropy, out_top_token, out_top_logprob, status   as above
+ *   out_logprob, status [B][L + 1], out_entropy, out_top_token, out_top_logprob   as above
  * accepted_len[b] outside [0, L] leaves all slots of the sequence empty.
  */
 int rsd_emitted_logprobs(const rsd_rows* target, int B, int num_nodes, int V, int L, const int32_t* accepted_len,
@@ -347,6 +347,7 @@ int rsd_emitted_logprobs(const rsd_rows* target, int B, int num_nodes, int V, in
  * an absent one not at all; entries without probability get what the formula gives at p_x = 0; a row without entries gets 0 throughout.
  *   rows [B][R][V];  token [B][R][T], 1 <= T <= RSD_MAX_K;  grad_logprob [B][R][T], grad_entropy optional [B][R], fp32
  *   grad_rows    [B][R][V] dense, the rows' element type, rounded once; may not overlap the rows
+ *   status       [B][R]
  */
 int rsd_token_logprobs_backward(const rsd_rows* rows, int B, int R, int V, const int32_t* token, int T, const float* grad_logprob,
                                 const float* grad_entropy, void* grad_rows, int32_t* status, rsd_stream_t stream);
@@ -360,7 +361,7 @@ int rsd_token_logprobs_backward(const rsd_rows* rows, int B, int R, int V, const
  * tree), so that the target may have more rows.  Terms with weight 0 are 0; a weight below 2^-126 of its row's largest counts as 0.  A token
  * with mass in one row only makes the divergence from that row infinite (RSD_ST_ZERO_DRAFT_PROB, RSD_ST_ZERO_TARGET_PROB).  NaN
  * and +inf entries count as -inf (RSD_ST_NAN_INPUT); where either row has no entry all three are 0 (RSD_ST_EMPTY_ROW).
- * draft and target must have the same dtype.  The outputs have the same bits in every launch.
+ * draft and target must have the same dtype.  The outputs have the same bits in every launch.  status [B][R].
  */
 int rsd_row_divergence(const rsd_rows* draft, const rsd_rows* target, int B, int R, int V, float* out_kl, float* out_reverse_kl,
                        float* out_overlap, int32_t* status, rsd_stream_t stream);
@@ -368,7 +369,8 @@ int rsd_row_divergence(const rsd_rows* draft, const rsd_rows* target, int B, int
 /*
  * Gradient of  grad_kl[b][r] KL(q||p) + grad_reverse_kl[b][r] KL(p||q)  with respect to the stored values of the draft rows:
  *   ( g (p_x - q_x) + h p_x (ln p_x - ln q_x - KL(p||q)) ) / T_draft
- * (either may be NULL, not both).  A row whose KL(p||q) is infinite gets no gradient of it; a pair of rows of which one has no entry gets 0.
+ * (either may be NULL, not both).  A row whose KL(p||q) is infinite gets no gradient of it (RSD_ST_ZERO_TARGET_PROB); a pair of rows of
+ * which one has no entry gets 0 (RSD_ST_EMPTY_ROW).  status [B][R].
  *   grad_draft   [B][R][V] dense, the rows' element type, rounded once; may not overlap the rows
  */
 int rsd_row_divergence_backward(const rsd_rows* draft, const rsd_rows* target, int B, int R, int V, const float* grad_kl,

@@ -310,77 +310,49 @@ def rsd_resample_residual(draft_row: Optional[torch.Tensor], target_row: torch.T
     return dict(token=token, residual=residual, status=status)
 
 
+_plain_new = _new
+
+
+def _make():
+    """What allocates the outputs of a scoring call: the binding (None), or whatever stands in `_new`'s place."""
+    return None if _new is _plain_new else _new
+
+
 def rsd_token_logprobs(rows: torch.Tensor, token: Optional[torch.Tensor] = None, *, top_k: int = 0, row_index: Optional[torch.Tensor] = None,
                        want_entropy: bool = True, temperature: float = 1.0, out: Optional[dict] = None):
     """rows [B, N, V], token [B, R] or [B, R, T] int32 (-1: absent) or None, row_index [B, R] int32 or None (slot r is row r) -> dict(logprob of
-    token's shape, entropy [B, R], top_token and top_logprob [B, R, top_k], status [B]); None where not asked for.  logprob is 0 for an
+    token's shape, entropy [B, R], top_token and top_logprob [B, R, top_k], status [B, R]); None where not asked for.  logprob is 0 for an
     absent token or slot.  For gradients see rsd_token_logprobs_backward."""
-    if out is None:
-        B, R, V = rows.shape
-        dev = rows.device
-        given = token if row_index is None else row_index
-        if given is not None and given.dim() > 1:
-            R = given.shape[1]
-        out = dict(logprob=None if token is None else _new(tuple(token.shape), torch.float32, dev),
-                   entropy=_new((B, R), torch.float32, dev) if want_entropy else None,
-                   top_token=_new((B, R, top_k), torch.int32, dev) if top_k else None,
-                   top_logprob=_new((B, R, top_k), torch.float32, dev) if top_k else None,
-                   status=_new((B,), torch.int32, dev))
-    (_native or _bind()).token_logprobs(rows, temperature, row_index, token, top_k, out.get("logprob"), out.get("entropy"), out.get("top_token"),
-                                        out.get("top_logprob"), out["status"])
-    return out
+    return (_native or _bind()).token_logprobs(rows, temperature, row_index, token, top_k, want_entropy, out, _make())
 
 
 def rsd_emitted_logprobs(target: torch.Tensor, verified: dict, *, top_k: int = 0, want_entropy: bool = True, temperature: float = 1.0,
                          out: Optional[dict] = None):
     """target [B, N+1, V] and what rsd_verify_tree returned for it -> dict(token, logprob, entropy [B, L+1], top_token and top_logprob
-    [B, L+1, top_k], status [B]): the tokens that the step emitted, in order, scored on the target rows that they were tested on or drawn
+    [B, L+1, top_k], status [B, L+1]): the tokens that the step emitted, in order, scored on the target rows that they were tested on or drawn
     from.  Slots beyond accepted_len + 1 hold -1, 0, 0, -1, -inf.  Only the visited rows are read."""
-    node, tok = verified["accepted_node"], verified["accepted_token"]
-    if out is None:
-        B, N1, V = target.shape
-        L, dev = node.shape[-1], target.device
-        out = dict(token=_new((B, L + 1), torch.int32, dev), logprob=_new((B, L + 1), torch.float32, dev),
-                   entropy=_new((B, L + 1), torch.float32, dev) if want_entropy else None,
-                   top_token=_new((B, L + 1, top_k), torch.int32, dev) if top_k else None,
-                   top_logprob=_new((B, L + 1, top_k), torch.float32, dev) if top_k else None,
-                   status=_new((B,), torch.int32, dev))
-    (_native or _bind()).emitted_logprobs(target, temperature, verified["accepted_len"], node, tok, verified["last_token"], top_k, out.get("token"),
-                                          out["logprob"], out.get("entropy"), out.get("top_token"), out.get("top_logprob"), out["status"])
-    return out
+    return (_native or _bind()).emitted_logprobs(target, temperature, verified["accepted_len"], verified["accepted_node"], verified["accepted_token"],
+                                                 verified["last_token"], top_k, want_entropy, out, _make())
 
 
 def rsd_token_logprobs_backward(rows: torch.Tensor, token: torch.Tensor, grad_logprob: torch.Tensor, grad_entropy: Optional[torch.Tensor] = None, *,
                                 temperature: float = 1.0, out: Optional[dict] = None):
     """rows [B, R, V], token and grad_logprob [B, R] or [B, R, T], grad_entropy [B, R] or None -> dict(grad_rows [B, R, V] in the rows' dtype,
-    status [B]): the gradient of sum grad_logprob * logprob + sum grad_entropy * entropy with respect to the rows.  Where the rows come
+    status [B, R]): the gradient of sum grad_logprob * logprob + sum grad_entropy * entropy with respect to the rows.  Where the rows come
     out of a model, `rows.backward(grad_rows)` carries it on."""
-    if out is None:
-        out = dict(grad_rows=_new(tuple(rows.shape), rows.dtype, rows.device), status=_new((rows.shape[0],), torch.int32, rows.device))
-    (_native or _bind()).token_logprobs_backward(rows, temperature, token, grad_logprob, grad_entropy, out["grad_rows"], out["status"])
-    return out
+    return (_native or _bind()).token_logprobs_backward(rows, temperature, token, grad_logprob, grad_entropy, out, _make())
 
 
 def rsd_row_divergence(draft: torch.Tensor, target: torch.Tensor, *, want_kl: bool = True, want_reverse_kl: bool = True, want_overlap: bool = True,
                        draft_temperature: float = 1.0, target_temperature: float = 1.0, out: Optional[dict] = None):
-    """draft [B, R, V], target [B, >= R, V] -> dict(kl = KL(target || draft), reverse_kl = KL(draft || target), overlap = sum min(p, q) [B, R],
-    status [B]); None where not asked for.  For gradients see rsd_row_divergence_backward."""
-    if out is None:
-        shape, dev = tuple(draft.shape[:2]), draft.device
-        out = dict(kl=_new(shape, torch.float32, dev) if want_kl else None, reverse_kl=_new(shape, torch.float32, dev) if want_reverse_kl else None,
-                   overlap=_new(shape, torch.float32, dev) if want_overlap else None, status=_new(shape[:1], torch.int32, dev))
-    (_native or _bind()).row_divergence(draft, draft_temperature, target, target_temperature, out.get("kl"), out.get("reverse_kl"), out.get("overlap"),
-                                        out["status"])
-    return out
+    """draft [B, R, V], target [B, >= R, V] -> dict(kl = KL(target || draft), reverse_kl = KL(draft || target), overlap = sum min(p, q), status
+    [B, R]); None where not asked for.  For gradients see rsd_row_divergence_backward."""
+    return (_native or _bind()).row_divergence(draft, draft_temperature, target, target_temperature, want_kl, want_reverse_kl, want_overlap, out, _make())
 
 
 def rsd_row_divergence_backward(draft: torch.Tensor, target: torch.Tensor, grad_kl: Optional[torch.Tensor] = None,
                                 grad_reverse_kl: Optional[torch.Tensor] = None, *, draft_temperature: float = 1.0, target_temperature: float = 1.0,
                                 out: Optional[dict] = None):
     """draft [B, R, V], target [B, >= R, V], grad_kl and grad_reverse_kl [B, R] (one may be None) -> dict(grad_draft [B, R, V] in the rows' dtype,
-    status [B]): the gradient of sum grad_kl * kl + sum grad_reverse_kl * reverse_kl with respect to the draft rows."""
-    if out is None:
-        out = dict(grad_draft=_new(tuple(draft.shape), draft.dtype, draft.device), status=_new((draft.shape[0],), torch.int32, draft.device))
-    (_native or _bind()).row_divergence_backward(draft, draft_temperature, target, target_temperature, grad_kl, grad_reverse_kl, out["grad_draft"],
-                                                 out["status"])
-    return out
+    status [B, R]): the gradient of sum grad_kl * kl + sum grad_reverse_kl * reverse_kl with respect to the draft rows."""
+    return (_native or _bind()).row_divergence_backward(draft, draft_temperature, target, target_temperature, grad_kl, grad_reverse_kl, out, _make())

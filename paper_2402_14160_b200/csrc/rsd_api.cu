@@ -102,12 +102,11 @@ __global__ void clear_status_kernel(int32_t* status, int B) {
     const int i = blockIdx.x * blockDim.x + threadIdx.x;
     if (i < B) status[i] = 0;
 }
+void clear_status(int32_t* status, int B, cudaStream_t s) { clear_status_kernel<<<(B + 255) / 256, 256, 0, s>>>(status, B); }
 
 size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 }  // namespace
-
-void rsd_host::clear_status(int32_t* status, int B, cudaStream_t s) { clear_status_kernel<<<(B + 255) / 256, 256, 0, s>>>(status, B); }
 
 extern "C" {
 

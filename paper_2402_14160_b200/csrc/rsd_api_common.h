@@ -48,9 +48,6 @@ inline void launch_overlapped(void (*kernel)(KArgs...), unsigned blocks, unsigne
     cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
-// Clears status[0..B) ahead of a kernel that ORs bits into it (in rsd_api.cu).
-void clear_status(int32_t* status, int B, cudaStream_t s);
-
 // SMs of the current device (asked once per device; 148 if the query fails)
 inline int sm_count() {
     static std::atomic<int> known[64];

@@ -27,7 +27,6 @@ rsd::ScoreArgs score_args(const rsd_rows* rows, int R, int V, int T, int K) {
     a.data = rows->data; a.seq_stride = rows->seq_stride; a.row_stride = rows->row_stride;
     a.R = R; a.V = V; a.T = T; a.K = K;
     a.temp = temperature_of(rows); a.k = exponent_scale(a.temp);
-    a.own_status = R == 1;
     return a;
 }
 rsd::DivergenceArgs divergence_args(const rsd_rows* draft, const rsd_rows* target, int R, int V) {
@@ -38,7 +37,6 @@ rsd::DivergenceArgs divergence_args(const rsd_rows* draft, const rsd_rows* targe
     a.R = R; a.V = V;
     a.draft_temp = temperature_of(draft);
     a.k_draft = exponent_scale(a.draft_temp); a.k_target = exponent_scale(temperature_of(target));
-    a.own_status = R == 1;
     return a;
 }
 int check_pair(const rsd_rows* draft, const rsd_rows* target, int B, int R, int V) {
@@ -52,7 +50,6 @@ int check_pair(const rsd_rows* draft, const rsd_rows* target, int B, int R, int 
 }
 
 int launch_scores(const rsd_rows* rows, int B, const rsd::ScoreArgs& a, cudaStream_t s, const char* what) {
-    if (!a.own_status) clear_status(a.status, B, s);
     const unsigned slots = (unsigned)((int64_t)B * a.R);
     if (rows->dtype == RSD_F32) rsd::launch_score_f32(rows_aligned(rows), slots, a, s);
     else rsd::launch_score_bf16(rows_aligned(rows), slots, a, s);
@@ -119,7 +116,6 @@ int rsd_token_logprobs_backward(const rsd_rows* rows, int B, int R, int V, const
     cudaStream_t s = (cudaStream_t)stream;
     rsd::ScoreArgs a = score_args(rows, R, V, T, 0);
     a.num_rows = R; a.token = token; a.g_logprob = grad_logprob; a.g_entropy = grad_entropy; a.grad = grad_rows; a.status = status;
-    if (!a.own_status) clear_status(status, B, s);
     const bool aligned = rows_aligned(rows) && dense_aligned(grad_rows, V, rows->dtype);
     const unsigned slots = (unsigned)((int64_t)B * R);
     if (rows->dtype == RSD_F32) rsd::launch_score_grad_f32(aligned, slots, a, s);
@@ -136,7 +132,6 @@ int rsd_row_divergence(const rsd_rows* draft, const rsd_rows* target, int B, int
     cudaStream_t s = (cudaStream_t)stream;
     rsd::DivergenceArgs a = divergence_args(draft, target, R, V);
     a.out_kl = out_kl; a.out_reverse = out_reverse_kl; a.out_overlap = out_overlap; a.status = status;
-    if (!a.own_status) clear_status(status, B, s);
     const bool aligned = rows_aligned(draft) && rows_aligned(target);
     const unsigned slots = (unsigned)((int64_t)B * R);
     if (draft->dtype == RSD_F32) rsd::launch_divergence_f32(aligned, slots, a, s);
@@ -153,7 +148,6 @@ int rsd_row_divergence_backward(const rsd_rows* draft, const rsd_rows* target, i
     cudaStream_t s = (cudaStream_t)stream;
     rsd::DivergenceArgs a = divergence_args(draft, target, R, V);
     a.g_kl = grad_kl; a.g_reverse = grad_reverse_kl; a.grad = grad_draft; a.status = status;
-    if (!a.own_status) clear_status(status, B, s);
     const bool aligned = rows_aligned(draft) && rows_aligned(target) && dense_aligned(grad_draft, V, draft->dtype);
     const unsigned slots = (unsigned)((int64_t)B * R);
     if (draft->dtype == RSD_F32) rsd::launch_divergence_grad_f32(aligned, slots, a, s);

@@ -4,13 +4,15 @@
 // on attribute look-ups and conversions, more than a small draft or walk takes on the GPU; this takes two to three.
 #include <Python.h>
 #include <dlfcn.h>
+#include <ATen/ops/empty.h>
+#include <torch/csrc/Device.h>
+#include <torch/csrc/DynamicTypes.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 
 #include <climits>
-#include <initializer_list>
 #include <vector>
 
 #include "../../include/rsd.h"
@@ -291,10 +293,16 @@ PyObject* resample_residual(PyObject* const* a) {
 }
 
 // ---- scoring of rows: every tensor is checked against the rows' device, its type and its shape --------------------------------------------
-// The data of a contiguous tensor of this type and shape on the rows' device (None: null where it may be left out).
-void* data_of(PyObject* o, const char* name, at::ScalarType type, const at::Tensor& rows, std::initializer_list<int64_t> shape, bool optional = false) {
-    if (o == Py_None && optional) return nullptr;
-    const at::Tensor& t = tensor(o);
+constexpr int kMostDims = 3;
+struct Shape {
+    int64_t n[kMostDims];
+    int dims;
+    at::IntArrayRef ref() const { return at::IntArrayRef(n, (size_t)dims); }
+};
+Shape shape_of(int64_t a, int64_t b) { return {{a, b, 0}, 2}; }
+Shape shape_of(int64_t a, int64_t b, int64_t c) { return {{a, b, c}, 3}; }
+
+void check_tensor(const at::Tensor& t, const char* name, at::ScalarType type, const at::Tensor& rows, const Shape& shape) {
     if (t.device() != rows.device()) {
         PyErr_Format(g_error, "%s must live on the rows' device", name);
         throw Failed();
@@ -303,12 +311,87 @@ void* data_of(PyObject* o, const char* name, at::ScalarType type, const at::Tens
         PyErr_Format(g_error, "%s must be contiguous %s", name, type == at::kInt ? "int32" : type == at::kFloat ? "float32" : "and of the rows' dtype");
         throw Failed();
     }
-    if (t.sizes() != at::IntArrayRef(shape)) {
+    if (t.sizes() != shape.ref()) {
         PyErr_Format(g_error, "%s has the wrong shape", name);
         throw Failed();
     }
+}
+// The data of an input (None: null where it may be left out).
+const void* data_of(PyObject* o, const char* name, at::ScalarType type, const at::Tensor& rows, const Shape& shape, bool optional = false) {
+    if (o == Py_None && optional) return nullptr;
+    const at::Tensor& t = tensor(o);
+    check_tensor(t, name, type, rows, shape);
     return t.data_ptr();
 }
+
+// The outputs of a call: the caller's dict, or a new one.  Allocating them here takes a quarter of the time that it takes in Python (2.3 us a tensor there); `make`
+// is a function (shape, dtype, device) -> tensor to be used instead, or None.
+class Outputs {
+public:
+    Outputs(PyObject* given, PyObject* make, const at::Tensor& rows) : rows_(rows), make_(make) {
+        own_ = given == Py_None;
+        if (!own_ && !PyDict_Check(given)) {
+            PyErr_SetString(PyExc_TypeError, "out must be a dict");
+            throw Failed();
+        }
+        if (own_) dict_ = PyDict_New();
+        else Py_INCREF(dict_ = given);
+        if (!dict_) throw Failed();
+    }
+    ~Outputs() { Py_XDECREF(dict_); }
+    Outputs(const Outputs&) = delete;
+    Outputs& operator=(const Outputs&) = delete;
+
+    // want: the output is due in a new dict; must: it may not be missing from the caller's
+    void* get(const char* name, at::ScalarType type, const Shape& shape, bool want, bool must) {
+        if (own_) {
+            PyObject* o = want ? fresh(type, shape) : Py_NewRef(Py_None);
+            const int bad = o ? PyDict_SetItemString(dict_, name, o) : -1;
+            void* p = !bad && want ? THPVariable_Unpack(o).data_ptr() : nullptr;
+            Py_XDECREF(o);
+            if (bad) throw Failed();
+            return p;
+        }
+        PyObject* o = PyDict_GetItemString(dict_, name);
+        if (!o || o == Py_None) {
+            if (must) {
+                PyErr_Format(g_error, "out lacks %s", name);
+                throw Failed();
+            }
+            return nullptr;
+        }
+        const at::Tensor& t = tensor(o);
+        check_tensor(t, name, type, rows_, shape);
+        return t.data_ptr();
+    }
+    PyObject* done(PyObject* result) {   // result: what the call returned
+        if (!result) return nullptr;
+        Py_DECREF(result);
+        return Py_NewRef(dict_);
+    }
+
+private:
+    PyObject* fresh(at::ScalarType type, const Shape& shape) {
+        if (make_ == Py_None) return THPVariable_Wrap(at::empty(shape.ref(), rows_.options().dtype(type).requires_grad(false)));
+        PyObject* sizes = PyTuple_New(shape.dims);
+        if (!sizes) return nullptr;
+        for (int i = 0; i < shape.dims; ++i) PyTuple_SET_ITEM(sizes, i, PyLong_FromLongLong(shape.n[i]));
+        PyObject *dtype = (PyObject*)torch::getTHPDtype(type), *device = THPDevice_New(rows_.device());
+        PyObject* o = device ? PyObject_CallFunctionObjArgs(make_, sizes, dtype, device, nullptr) : nullptr;
+        Py_XDECREF(device);
+        Py_DECREF(sizes);
+        if (o && !THPVariable_Check(o)) {
+            Py_DECREF(o);
+            PyErr_SetString(PyExc_TypeError, "a tensor is expected");
+            return nullptr;
+        }
+        return o;
+    }
+    const at::Tensor& rows_;
+    PyObject *make_, *dict_ = nullptr;
+    bool own_;
+};
+
 struct Batch {
     int B, R, V;
 };
@@ -318,39 +401,59 @@ Batch batch_of(const at::Tensor& t) {
         if (t.size(i) > INT_MAX) fail("rows: too many of them");
     return {(int)t.size(0), (int)t.size(1), (int)t.size(2)};
 }
+int limited(int64_t n, const char* message) {
+    if (n > INT_MAX) fail(message);
+    return (int)n;
+}
+// Given tokens: [B, R], one a slot, or [B, R, T].
+struct Tokens {
+    int R, T;
+    Shape shape;
+};
+Tokens tokens_of(PyObject* o, const Batch& n, int R) {
+    if (o == Py_None) return {R, 0, shape_of(n.B, R)};
+    const at::Tensor& t = tensor(o);
+    if (t.dim() == 2) return {limited(t.size(1), "token: too many of them"), 1, shape_of(n.B, t.size(1))};
+    want_dims(t, 3);
+    return {limited(t.size(1), "token: too many of them"), limited(t.size(2), "token: too many of them"), shape_of(n.B, t.size(1), t.size(2))};
+}
+int alternatives(PyObject* o) {   // (before outputs of that size are made)
+    const long long K = integer(o);
+    if (K < 0 || K > RSD_MAX_K) {
+        PyErr_Format(g_error, "K = %lld outside [0, %d]", K, (int)RSD_MAX_K);
+        throw Failed();
+    }
+    return (int)K;
+}
 
-// rows, temperature, row_index, token, K, logprob, entropy, top_token, top_logprob, status
+// rows, temperature, row_index, token, K, want_entropy, out, make
 PyObject* token_logprobs(PyObject* const* a) {
     const at::Tensor& t = tensor(a[0]);
     const Batch n = batch_of(t);
     const rsd_rows r = rows_of(t, false, real(a[1]));
-    const int K = (int)integer(a[4]);
-    int64_t R = n.R, T = 0;
-    const bool flat = a[3] != Py_None && tensor(a[3]).dim() == 2;    // one token a slot, without a dimension of its own
+    const int K = alternatives(a[4]);
+    int R = n.R;
     if (a[2] != Py_None) {
         want_dims(tensor(a[2]), 2);
-        R = tensor(a[2]).size(1);
+        R = limited(tensor(a[2]).size(1), "row_index: too many slots");
     }
-    if (a[3] != Py_None) {
-        if (!flat) want_dims(tensor(a[3]), 3);
-        T = flat ? 1 : tensor(a[3]).size(2);
-        if (a[2] == Py_None) R = tensor(a[3]).size(1);
-    }
-    if (R > INT_MAX || T > INT_MAX) fail("token: too many of them");
-    const int32_t* index = (const int32_t*)data_of(a[2], "row_index", at::kInt, t, {n.B, R}, true);
-    const int32_t* token = (const int32_t*)(flat ? data_of(a[3], "token", at::kInt, t, {n.B, R}) : data_of(a[3], "token", at::kInt, t, {n.B, R, T}, true));
-    float* logprob = (float*)(flat ? data_of(a[5], "logprob", at::kFloat, t, {n.B, R}) : data_of(a[5], "logprob", at::kFloat, t, {n.B, R, T}, T == 0));
-    float* entropy = (float*)data_of(a[6], "entropy", at::kFloat, t, {n.B, R}, true);
-    int32_t* top_token = (int32_t*)data_of(a[7], "top_token", at::kInt, t, {n.B, R, K}, K == 0);
-    float* top_logprob = (float*)data_of(a[8], "top_logprob", at::kFloat, t, {n.B, R, K}, K == 0);
-    int32_t* status = (int32_t*)data_of(a[9], "status", at::kInt, t, {n.B});
-    if (n.B == 0) Py_RETURN_NONE;
+    const Tokens k = tokens_of(a[3], n, R);
+    if (a[2] == Py_None) R = k.R;
+    else if (k.R != R) fail("token has the wrong shape");
+    const int32_t *index = (const int32_t*)data_of(a[2], "row_index", at::kInt, t, shape_of(n.B, R), true), *token = (const int32_t*)data_of(a[3], "token", at::kInt, t, k.shape, true);
     const c10::cuda::CUDAGuard device(t.device());
+    Outputs out(a[6], a[7], t);
+    float* logprob = (float*)out.get("logprob", at::kFloat, k.shape, a[3] != Py_None, k.T > 0);
+    float* entropy = (float*)out.get("entropy", at::kFloat, shape_of(n.B, R), truth(a[5]), false);
+    int32_t* top_token = (int32_t*)out.get("top_token", at::kInt, shape_of(n.B, R, K), K > 0, K > 0);
+    float* top_logprob = (float*)out.get("top_logprob", at::kFloat, shape_of(n.B, R, K), K > 0, K > 0);
+    int32_t* status = (int32_t*)out.get("status", at::kInt, shape_of(n.B, R), true, true);
+    if (n.B == 0) return out.done(Py_NewRef(Py_None));
     const rsd_stream_t s = stream();
-    return call([&] { return p_token_logprobs(&r, n.B, (int)R, n.V, n.R, index, token, (int)T, K, logprob, entropy, top_token, top_logprob, status, s); });
+    return out.done(call([&] { return p_token_logprobs(&r, n.B, R, n.V, n.R, index, token, k.T, K, logprob, entropy, top_token, top_logprob, status, s); }));
 }
 
-// target, temperature, accepted_len, accepted_node, accepted_token, last_token, K, token, logprob, entropy, top_token, top_logprob, status
+// target, temperature, accepted_len, accepted_node, accepted_token, last_token, K, want_entropy, out, make
 PyObject* emitted_logprobs(PyObject* const* a) {
     const at::Tensor& t = tensor(a[0]);
     const Batch n = batch_of(t);
@@ -358,40 +461,42 @@ PyObject* emitted_logprobs(PyObject* const* a) {
     want_dims(tensor(a[3]), 2);
     const int64_t L = tensor(a[3]).size(1);
     if (L >= RSD_MAX_TREE_NODES) fail("accepted_node: too many levels");
-    const int K = (int)integer(a[6]);
-    const int32_t *len = (const int32_t*)data_of(a[2], "accepted_len", at::kInt, t, {n.B}), *node = (const int32_t*)data_of(a[3], "accepted_node", at::kInt, t, {n.B, L}),
-                  *tok = (const int32_t*)data_of(a[4], "accepted_token", at::kInt, t, {n.B, L}), *last = (const int32_t*)data_of(a[5], "last_token", at::kInt, t, {n.B});
-    int32_t* token = (int32_t*)data_of(a[7], "token", at::kInt, t, {n.B, L + 1}, true);
-    float *logprob = (float*)data_of(a[8], "logprob", at::kFloat, t, {n.B, L + 1}), *entropy = (float*)data_of(a[9], "entropy", at::kFloat, t, {n.B, L + 1}, true);
-    int32_t* top_token = (int32_t*)data_of(a[10], "top_token", at::kInt, t, {n.B, L + 1, K}, K == 0);
-    float* top_logprob = (float*)data_of(a[11], "top_logprob", at::kFloat, t, {n.B, L + 1, K}, K == 0);
-    int32_t* status = (int32_t*)data_of(a[12], "status", at::kInt, t, {n.B});
-    if (n.B == 0) Py_RETURN_NONE;
+    const int K = alternatives(a[6]);
+    const at::Tensor &len_t = tensor(a[2]), &last_t = tensor(a[5]);
+    const Shape one = {{n.B, 0, 0}, 1}, slots = shape_of(n.B, L + 1);
+    check_tensor(len_t, "accepted_len", at::kInt, t, one), check_tensor(last_t, "last_token", at::kInt, t, one);
+    const int32_t *len = (const int32_t*)len_t.data_ptr(), *last = (const int32_t*)last_t.data_ptr();
+    const int32_t *node = (const int32_t*)data_of(a[3], "accepted_node", at::kInt, t, shape_of(n.B, L)), *tok = (const int32_t*)data_of(a[4], "accepted_token", at::kInt, t, shape_of(n.B, L));
     const c10::cuda::CUDAGuard device(t.device());
+    Outputs out(a[8], a[9], t);
+    int32_t* token = (int32_t*)out.get("token", at::kInt, slots, true, false);
+    float *logprob = (float*)out.get("logprob", at::kFloat, slots, true, true), *entropy = (float*)out.get("entropy", at::kFloat, slots, truth(a[7]), false);
+    int32_t* top_token = (int32_t*)out.get("top_token", at::kInt, shape_of(n.B, L + 1, K), K > 0, K > 0);
+    float* top_logprob = (float*)out.get("top_logprob", at::kFloat, shape_of(n.B, L + 1, K), K > 0, K > 0);
+    int32_t* status = (int32_t*)out.get("status", at::kInt, slots, true, true);
+    if (n.B == 0) return out.done(Py_NewRef(Py_None));
     const rsd_stream_t s = stream();
-    return call([&] {
-        return p_emitted_logprobs(&r, n.B, n.R, n.V, (int)L, len, node, tok, last, K, token, logprob, entropy, top_token, top_logprob, status, s);
-    });
+    return out.done(
+        call([&] { return p_emitted_logprobs(&r, n.B, n.R, n.V, (int)L, len, node, tok, last, K, token, logprob, entropy, top_token, top_logprob, status, s); }));
 }
 
-// rows, temperature, token, grad_logprob, grad_entropy, grad_rows, status
+// rows, temperature, token, grad_logprob, grad_entropy, out, make
 PyObject* token_logprobs_backward(PyObject* const* a) {
-    const at::Tensor &t = tensor(a[0]), &tok = tensor(a[2]);
+    const at::Tensor& t = tensor(a[0]);
     const Batch n = batch_of(t);
     const rsd_rows r = rows_of(t, false, real(a[1]));
-    const bool flat = tok.dim() == 2;
-    if (!flat) want_dims(tok, 3);
-    const int64_t T = flat ? 1 : tok.size(2);
-    if (T > INT_MAX) fail("token: too many of them");
-    const int32_t* token = (const int32_t*)(flat ? data_of(a[2], "token", at::kInt, t, {n.B, n.R}) : data_of(a[2], "token", at::kInt, t, {n.B, n.R, T}));
-    const float* g = (const float*)(flat ? data_of(a[3], "grad_logprob", at::kFloat, t, {n.B, n.R}) : data_of(a[3], "grad_logprob", at::kFloat, t, {n.B, n.R, T}));
-    const float* h = (const float*)data_of(a[4], "grad_entropy", at::kFloat, t, {n.B, n.R}, true);
-    void* grad = data_of(a[5], "grad_rows", t.scalar_type(), t, {n.B, n.R, n.V});
-    int32_t* status = (int32_t*)data_of(a[6], "status", at::kInt, t, {n.B});
-    if (n.B == 0) Py_RETURN_NONE;
+    tensor(a[2]);                                    // (not None)
+    const Tokens k = tokens_of(a[2], n, n.R);
+    if (k.R != n.R) fail("token has the wrong shape");
+    const int32_t* token = (const int32_t*)data_of(a[2], "token", at::kInt, t, k.shape);
+    const float *g = (const float*)data_of(a[3], "grad_logprob", at::kFloat, t, k.shape), *h = (const float*)data_of(a[4], "grad_entropy", at::kFloat, t, shape_of(n.B, n.R), true);
     const c10::cuda::CUDAGuard device(t.device());
+    Outputs out(a[5], a[6], t);
+    void* grad = out.get("grad_rows", t.scalar_type(), shape_of(n.B, n.R, n.V), true, true);
+    int32_t* status = (int32_t*)out.get("status", at::kInt, shape_of(n.B, n.R), true, true);
+    if (n.B == 0) return out.done(Py_NewRef(Py_None));
     const rsd_stream_t s = stream();
-    return call([&] { return p_token_logprobs_backward(&r, n.B, n.R, n.V, token, (int)T, g, h, grad, status, s); });
+    return out.done(call([&] { return p_token_logprobs_backward(&r, n.B, n.R, n.V, token, k.T, g, h, grad, status, s); }));
 }
 
 // The target rows that belong to a batch of draft rows: as many sequences, at least as many rows, as long.
@@ -401,34 +506,38 @@ void check_pair(const at::Tensor& target, const at::Tensor& draft, const Batch& 
     if (m.B != n.B || m.R < n.R || m.V != n.V) fail("target must hold the draft's sequences, at least as many rows of each, and rows as long");
 }
 
-// draft, draft temperature, target, target temperature, kl, reverse_kl, overlap, status
+// draft, draft temperature, target, target temperature, want_kl, want_reverse_kl, want_overlap, out, make
 PyObject* row_divergence(PyObject* const* a) {
     const at::Tensor &d = tensor(a[0]), &t = tensor(a[2]);
     const Batch n = batch_of(d);
     check_pair(t, d, n);
     const rsd_rows dr = rows_of(d, false, real(a[1])), tr = rows_of(t, false, real(a[3]));
-    float *kl = (float*)data_of(a[4], "kl", at::kFloat, d, {n.B, n.R}, true), *reverse = (float*)data_of(a[5], "reverse_kl", at::kFloat, d, {n.B, n.R}, true),
-          *overlap = (float*)data_of(a[6], "overlap", at::kFloat, d, {n.B, n.R}, true);
-    int32_t* status = (int32_t*)data_of(a[7], "status", at::kInt, d, {n.B});
-    if (n.B == 0) Py_RETURN_NONE;
     const c10::cuda::CUDAGuard device(d.device());
+    Outputs out(a[7], a[8], d);
+    const Shape slots = shape_of(n.B, n.R);
+    float *kl = (float*)out.get("kl", at::kFloat, slots, truth(a[4]), false), *reverse = (float*)out.get("reverse_kl", at::kFloat, slots, truth(a[5]), false),
+          *overlap = (float*)out.get("overlap", at::kFloat, slots, truth(a[6]), false);
+    int32_t* status = (int32_t*)out.get("status", at::kInt, slots, true, true);
+    if (n.B == 0) return out.done(Py_NewRef(Py_None));
     const rsd_stream_t s = stream();
-    return call([&] { return p_row_divergence(&dr, &tr, n.B, n.R, n.V, kl, reverse, overlap, status, s); });
+    return out.done(call([&] { return p_row_divergence(&dr, &tr, n.B, n.R, n.V, kl, reverse, overlap, status, s); }));
 }
 
-// draft, draft temperature, target, target temperature, grad_kl, grad_reverse_kl, grad_draft, status
+// draft, draft temperature, target, target temperature, grad_kl, grad_reverse_kl, out, make
 PyObject* row_divergence_backward(PyObject* const* a) {
     const at::Tensor &d = tensor(a[0]), &t = tensor(a[2]);
     const Batch n = batch_of(d);
     check_pair(t, d, n);
     const rsd_rows dr = rows_of(d, false, real(a[1])), tr = rows_of(t, false, real(a[3]));
-    const float *g = (const float*)data_of(a[4], "grad_kl", at::kFloat, d, {n.B, n.R}, true), *h = (const float*)data_of(a[5], "grad_reverse_kl", at::kFloat, d, {n.B, n.R}, true);
-    void* grad = data_of(a[6], "grad_draft", d.scalar_type(), d, {n.B, n.R, n.V});
-    int32_t* status = (int32_t*)data_of(a[7], "status", at::kInt, d, {n.B});
-    if (n.B == 0) Py_RETURN_NONE;
+    const Shape slots = shape_of(n.B, n.R);
+    const float *g = (const float*)data_of(a[4], "grad_kl", at::kFloat, d, slots, true), *h = (const float*)data_of(a[5], "grad_reverse_kl", at::kFloat, d, slots, true);
     const c10::cuda::CUDAGuard device(d.device());
+    Outputs out(a[6], a[7], d);
+    void* grad = out.get("grad_draft", d.scalar_type(), shape_of(n.B, n.R, n.V), true, true);
+    int32_t* status = (int32_t*)out.get("status", at::kInt, slots, true, true);
+    if (n.B == 0) return out.done(Py_NewRef(Py_None));
     const rsd_stream_t s = stream();
-    return call([&] { return p_row_divergence_backward(&dr, &tr, n.B, n.R, n.V, g, h, grad, status, s); });
+    return out.done(call([&] { return p_row_divergence_backward(&dr, &tr, n.B, n.R, n.V, g, h, grad, status, s); }));
 }
 
 // bind(path of librsd, exception class)
@@ -490,10 +599,10 @@ PyMethodDef methods[] = {
     RSD_ENTRY(sbs_draft_tree, 15),
     RSD_ENTRY(verify_tree, 21),
     RSD_ENTRY(resample_residual, 12),
-    RSD_ENTRY(token_logprobs, 10),
-    RSD_ENTRY(emitted_logprobs, 13),
+    RSD_ENTRY(token_logprobs, 8),
+    RSD_ENTRY(emitted_logprobs, 10),
     RSD_ENTRY(token_logprobs_backward, 7),
-    RSD_ENTRY(row_divergence, 8),
+    RSD_ENTRY(row_divergence, 9),
     RSD_ENTRY(row_divergence_backward, 8),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_rsdbind", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

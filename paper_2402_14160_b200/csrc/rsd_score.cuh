@@ -16,50 +16,47 @@ constexpr int kThreads = 256, kWarps = kThreads / 32, kWords = 8;
 constexpr int kMaxTiles = RSD_MAX_VOCAB / tiles::tile_entries<float>(kWords);
 constexpr int kBuckets = 64;       // samples that bound the K-th largest entry; at least RSD_MAX_K
 constexpr int kList = 512;         // groups opened, and entries taken from them
-static_assert(kBuckets >= RSD_MAX_K && kThreads % kBuckets == 0, "");
+static_assert(kBuckets == 64 && kBuckets >= RSD_MAX_K, "two buckets per lane");
 
-struct Sums {                      // of a row's tiles, relative to each tile's largest entry
+struct Sums {                      // of a row's tiles, relative to each tile's largest entry; every block of the row has all of them
     float m[kMaxTiles], s[kMaxTiles], w[kMaxTiles];
 };
 struct RowTotals {
     float m, s, w;                 // largest entry; sum of 2^y, of 2^y y
 };
 
-// Sum of 2^y and of 2^y y over a tile, y = (v - m) k; the largest entry in m (-inf: no entry at all).
+// Sum of 2^y and of 2^y y over a tile, y = (v - m) k, to all blocks of the row; lane_max: the lane's largest entry.
 template <typename T, bool ENTROPY>
-__device__ __forceinline__ void tile_sums(uint4 (&w)[kWords], float k, int t, int lane, Sums& sums, float& lane_max, bool& bad) {
+__device__ __forceinline__ void tile_sums(uint4 (&w)[kWords], float k, int t, int lane, uint32_t blocks, Sums& sums, float& lane_max, bool& bad) {
     using P = tiles::Packed16<T>;
-    float mx, mn;
-    P::bounds(w, mx, mn);
-    float m = tiles::warp_max_nan(mx);
-    if (!(m < __builtin_huge_valf())) {   // NaN or +inf somewhere in the tile
-#pragma unroll
-        for (int i = 0; i < kWords; ++i) P::clean(w[i], bad);
-        P::bounds(w, mx, mn);
-        m = tiles::warp_max_nan(mx);
-    }
-    lane_max = mx;
+    float mx = P::largest(w), m = tiles::warp_max_nan(mx);
     unsigned long long s = tiles::both(0.0f), e = s;
-    if (m > kNegInf) {
-        const unsigned long long minus_m = tiles::both(-m), kk = tiles::both(k);
-        const bool plain = (mn - m) * k > tiles::kFarBelow;
-        if (__all_sync(0xFFFFFFFFu, plain) || !ENTROPY) {
+    if (tiles::plain_tile(m, k)) {
+        const unsigned long long ref = tiles::both(-(m * k)), kk = tiles::both(k);
+#pragma unroll
+        for (int i = 0; i < kWords; ++i)
+            P::pairs(ENTROPY ? P::raised(w[i]) : w[i], [&](unsigned long long v) {
+                const unsigned long long y = fma_f32x2(v, kk, ref);
+                float a, b;
+                split_f32x2(y, a, b);
+                const unsigned long long x = f32x2(ex2_approx(a), ex2_approx(b));
+                s = add_f32x2(s, x);
+                if (ENTROPY) e = fma_f32x2(x, y, e);
+            });
+    } else {                                        // no entry, NaN, +inf, or values or a scale near the end of the range
+        if (!(m < __builtin_huge_valf())) {
+#pragma unroll
+            for (int i = 0; i < kWords; ++i) P::clean(w[i], bad);
+            mx = P::largest(w), m = tiles::warp_max_nan(mx);
+        }
+        if (m > kNegInf) {
+            const bool plain = tiles::plain_tile(m, k);   // (as the join takes it)
+            const unsigned long long minus_m = tiles::both(plain ? 0.0f : -m), ref = tiles::both(plain ? -(m * k) : 0.0f), kk = tiles::both(k);
 #pragma unroll
             for (int i = 0; i < kWords; ++i)
                 P::pairs(w[i], [&](unsigned long long v) {
-                    const unsigned long long y = tiles::mul_f32x2(add_f32x2(v, minus_m), kk);
                     float a, b;
-                    split_f32x2(y, a, b);
-                    const unsigned long long x = f32x2(ex2_approx(a), ex2_approx(b));
-                    s = add_f32x2(s, x);
-                    if (ENTROPY) e = fma_f32x2(x, y, e);
-                });
-        } else {
-#pragma unroll
-            for (int i = 0; i < kWords; ++i)
-                P::pairs(w[i], [&](unsigned long long v) {
-                    float a, b;
-                    split_f32x2(tiles::mul_f32x2(add_f32x2(v, minus_m), kk), a, b);
+                    split_f32x2(fma_f32x2(add_f32x2(v, minus_m), kk, ref), a, b);
                     a = fmaxf(a, tiles::kFarBelow), b = fmaxf(b, tiles::kFarBelow);
                     const unsigned long long x = f32x2(ex2_approx(a), ex2_approx(b));
                     s = add_f32x2(s, x);
@@ -67,12 +64,17 @@ __device__ __forceinline__ void tile_sums(uint4 (&w)[kWords], float k, int t, in
                 });
         }
     }
+    lane_max = mx;
     float s0, s1, e0, e1;
     split_f32x2(s, s0, s1);
     split_f32x2(e, e0, e1);
-    const float sum = tiles::warp_sum_two(s0 + s1, e0 + e1, lane);
-    if (lane == 0) sums.m[t] = m, sums.s[t] = sum;
-    if (lane == 16) sums.w[t] = sum;
+    const float sum = tiles::warp_sum_two(s0 + s1, e0 + e1, lane);   // lanes 0 to 15 the first, the others the second
+    const uint32_t to = lane & 7;
+    if (to < blocks) {
+        if (lane < 8) tiles::store_at(&sums.s[t], to, sum);
+        else if (lane < 16) tiles::store_at(&sums.m[t], to, m);
+        else if (lane < 24) tiles::store_at(&sums.w[t], to, sum);
+    }
 }
 
 // The tiles' sums joined by one warp; every lane gets the result.
@@ -82,8 +84,9 @@ __device__ __forceinline__ RowTotals join(const Sums& sums, int n, float k, int 
     m = warp_max(m);
     float s = 0.0f, w = 0.0f;
     for (int t = lane; t < n; t += 32) {
-        if (sums.m[t] == kNegInf) continue;
-        const float d = fmaxf((sums.m[t] - m) * k, tiles::kFarBelow), f = ex2_approx(d);
+        const float mt = sums.m[t];
+        if (mt == kNegInf) continue;
+        const float d = fmaxf((mt - m) * k, tiles::kFarBelow) - tiles::rounded_off(mt, k), f = ex2_approx(d);
         s = fmaf(f, sums.s[t], s);
         w = fmaf(f, fmaf(d, sums.s[t], sums.w[t]), w);
     }
@@ -98,16 +101,17 @@ __device__ __forceinline__ float entry(const void* row, int x) {   // -inf where
 }
 
 // ---- the K largest entries of a row ----------------------------------------------------------------------------------------------
-// Every lane knows its largest entry of each tile (a group of up to 64 entries).  The threads' largest entries, taken together into
-// kBuckets buckets, are distinct entries: the K-th largest of them is at most the K-th largest entry.  Only groups that reach it are read again (they lie in
-// L2), a word a thread, and only entries that reach it are ranked: about 1.4 K of them.
+// Every lane knows its largest entry of each tile (a group of up to 64 entries).  A block's largest entries per thread, taken together into
+// kBuckets buckets, are distinct entries: the K-th largest of them is at most the K-th largest entry of the row, and so is the largest such bound of
+// the row's blocks.  Only groups that reach their block's bound are read again (they lie in L2), a word a thread, and only entries that reach the row's are
+// ranked: about 1.4 K of them.
 struct TopSmem {
     float bucket[kThreads];
-    float value[kList];
-    int32_t token[kList];
+    float bound[tiles::kMaxBlocks];   // of every block of the row
     int32_t group[kList];
-    int groups, count;
-    float bound;
+    float all_value[kList];           // in the first block: the entries of all
+    int32_t all_token[kList];
+    int groups, all_count, overflow;
 };
 
 // K-th largest of 64 values, two per lane, from below: exact in its upper 16 bits.
@@ -124,12 +128,12 @@ __device__ __forceinline__ float bound_of_kth(float a, float b, int K) {
 
 // Beyond the list: the entries one after the other, each the best below the one before.
 template <typename T>
-__device__ void top_one_by_one(const void* row, int V, int K, TopSmem& sm, float* value, int32_t* token) {
+__device__ __noinline__ void top_one_by_one(const void* row, int V, int K, TopSmem& sm) {
     __shared__ float best_v[kWarps];
     __shared__ int best_x[kWarps];
     float last_v = __builtin_huge_valf();
-    int last_x = -1;
-    for (int i = 0; i < K; ++i) {
+    int last_x = -1, found = 0;
+    for (; found < K; ++found) {
         float v = kNegInf;
         int at = -1;
         for (int x = threadIdx.x; x < V; x += kThreads) {
@@ -150,63 +154,70 @@ __device__ void top_one_by_one(const void* row, int V, int K, TopSmem& sm, float
             if (best_x[j] >= 0 && (at < 0 || best_v[j] > v || (best_v[j] == v && best_x[j] < at))) v = best_v[j], at = best_x[j];
         if (at < 0) break;
         last_v = v, last_x = at;
-        if (threadIdx.x == 0) value[i] = v, token[i] = at, sm.count = i + 1;
+        if (threadIdx.x == 0) sm.all_value[found] = v, sm.all_token[found] = at;
     }
+    __syncthreads();
+    if (threadIdx.x == 0) sm.all_count = found;
     __syncthreads();
 }
 
-template <typename T, bool ALIGNED>
-__device__ void top_entries(const ScoreArgs& a, const void* row, const tiles::View& view, int n_tiles, float thread_max, const float* group_max, TopSmem& sm) {
-    using P = tiles::Packed16<T>;
+// Bound of a block, known to all blocks of the row behind the next barrier.
+__device__ __forceinline__ void block_bound(TopSmem& sm, float thread_max, int K, uint32_t rank, uint32_t blocks) {
     const int tid = threadIdx.x;
     sm.bucket[tid] = thread_max;
-    if (tid == 0) sm.groups = 0, sm.count = 0;
     __syncthreads();
     if (tid < 32) {
         float u = kNegInf, v = kNegInf;
 #pragma unroll
         for (int i = 0; i < kThreads; i += kBuckets) u = fmaxf(u, sm.bucket[i + tid]), v = fmaxf(v, sm.bucket[i + 32 + tid]);
-        const float b = bound_of_kth(u, v, a.K);
-        if (tid == 0) sm.bound = b;
+        const float b = bound_of_kth(u, v, K);
+        if ((uint32_t)tid < blocks) tiles::store_at(&sm.bound[rank], (uint32_t)tid, b);
     }
-    __syncthreads();
-    const float bound = sm.bound;
-    for (int i = tid; i < n_tiles * 32; i += kThreads)
+}
+
+// The entries of the block's tiles that reach the row's bound, in the first block's list.
+template <typename T, bool ALIGNED>
+__device__ __forceinline__ void gather_top(const ScoreArgs& a, const tiles::View& view, int n_groups, int first_tile, int tile_step, const float* group_max, TopSmem& sm,
+                                           uint32_t blocks) {
+    using P = tiles::Packed16<T>;
+    const int tid = threadIdx.x;
+    float bound = sm.bound[0];
+    for (uint32_t i = 1; i < blocks; ++i) bound = fmaxf(bound, sm.bound[i]);
+    for (int i = tid; i < n_groups; i += kThreads)
         if (group_max[i] >= bound && group_max[i] > kNegInf) {
             const int at = atomicAdd(&sm.groups, 1);
             if (at < kList) sm.group[at] = i;
         }
     __syncthreads();
     const int groups = sm.groups;
-    if (groups <= kList) {
+    if (groups > kList) {
+        if (tid == 0) tiles::store_at(&sm.overflow, 0, 1);
+    } else {
         for (int i = tid; i < groups * kWords; i += kThreads) {
-            const int g = sm.group[i / kWords], x0 = (((g >> 5) * kWords + i % kWords) * 32 + (g & 31)) * P::kEntries;
+            // group i: lane i & 31 of the block's (i >> 5)-th tile
+            const int g = sm.group[i / kWords], t = first_tile + (g >> 5) * tile_step, x0 = ((t * kWords + i % kWords) * 32 + (g & 31)) * P::kEntries;
             const uint4 w = tiles::load_word<T, ALIGNED>(view, x0, a.V);
 #pragma unroll
             for (int j = 0; j < P::kEntries; ++j) {
                 const float v = P::get(w, j);
                 if (v >= bound && v > kNegInf && v < __builtin_huge_valf()) {
-                    const int at = atomicAdd(&sm.count, 1);
-                    if (at < kList) sm.value[at] = v, sm.token[at] = x0 + j;
+                    const int at = tiles::add_at(&sm.all_count, 0, 1);
+                    if (at < kList) {
+                        tiles::store_at(&sm.all_value[at], 0, v);
+                        tiles::store_at(&sm.all_token[at], 0, x0 + j);
+                    }
                 }
             }
         }
     }
-    __syncthreads();
-    if (groups > kList || sm.count > kList) top_one_by_one<T>(row, a.V, a.K, sm, sm.value, sm.token);
 }
-
-struct Smem {
-    Sums sums;
-    RowTotals total;
-    int status;
-};
 
 // Row r of sequence b, and the token that the accepted path has there; false: the slot is empty.
 __device__ __forceinline__ bool slot_of(const ScoreArgs& a, int64_t slot, int64_t b, int r, const char*& row, int elem, int32_t& path_token, int& status) {
     int64_t at = r;
     bool there = true;
     path_token = -1;
+    row = nullptr;
     if (a.accepted_len) {
         const int len = a.accepted_len[b], L = a.R - 1;
         if (len < 0 || len > L || r > len) return false;
@@ -221,14 +232,23 @@ __device__ __forceinline__ bool slot_of(const ScoreArgs& a, int64_t slot, int64_
     return there;
 }
 
-template <typename T, bool ALIGNED>
-__global__ void __launch_bounds__(kThreads) score_rows_kernel(const __grid_constant__ ScoreArgs a) {
-    extern __shared__ float group_max[];           // [tiles][32] where the largest entries are asked for
-    __shared__ Smem sm;
-    __shared__ TopSmem top;
+// Tiles of a row are dealt to the warps of its blocks in turn: tile t to warp t / blocks mod kWarps of block t mod blocks.
+template <typename T, bool ALIGNED, bool TOP>
+__global__ void __launch_bounds__(kThreads, 3) score_rows_kernel(const __grid_constant__ ScoreArgs a) {
+    extern __shared__ float group_max[];           // [tiles of the block][32] where the largest entries are asked for
+    __shared__ Sums sums;
+    __shared__ RowTotals total_of_row;
+    __shared__ int status_of_row;
+    __shared__ typename std::conditional<TOP, TopSmem, int>::type top_store;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    if (a.own_status) grid_wait();                 // (otherwise the kernel ahead is the one that clears the status: waited for below)
-    const int64_t slot = blockIdx.x, b = slot / a.R;
+    const uint32_t rank = tiles::cluster_rank(), blocks = tiles::cluster_blocks();
+    if (tid == 0) {
+        status_of_row = 0;
+        if constexpr (TOP) top_store.groups = top_store.all_count = top_store.overflow = 0;
+    }
+    if (blocks > 1) tiles::cluster_arrive();       // (the row's other blocks have started, and their words above are set, behind the wait below)
+    grid_wait();
+    const int64_t slot = blockIdx.x / blocks, b = slot / a.R;
     const int r = (int)(slot - b * a.R);
     int status = 0;
     int32_t path_token;
@@ -236,79 +256,97 @@ __global__ void __launch_bounds__(kThreads) score_rows_kernel(const __grid_const
     const bool there = slot_of(a, slot, b, r, row, (int)sizeof(T), path_token, status);
     int32_t token = -1;
     float value = kNegInf;
-    if (tid < a.T) {
+    if (rank == 0 && tid < a.T) {
         token = a.accepted_len ? path_token : a.token ? a.token[slot * a.T + tid] : -1;
         if (token >= a.V) token = -1, status |= RSD_ST_BAD_INDEX;
         if (there && token >= 0) value = entry<T>(row, token);
     }
     const tiles::View view = tiles::view_of<T>(row, a.V);
     const int n_tiles = there ? tiles::tiles_of<T>(a.V, kWords) : 0;
-    if (tid == 0) sm.status = 0;
+    if (blocks > 1) tiles::cluster_wait();
+    else __syncthreads();
     float thread_max = kNegInf;
     bool bad = false;
-    for (int t = warp; t < n_tiles; t += kWarps) {
+    for (int i = warp, t = warp * (int)blocks + (int)rank; t < n_tiles; i += kWarps, t += kWarps * (int)blocks) {   // i: the tile's place in the block
         uint4 w[kWords];
         tiles::load_tile<T, ALIGNED, kWords>(w, view, t, lane, a.V);
         float lane_max;
-        tile_sums<T, true>(w, a.k, t, lane, sm.sums, lane_max, bad);
-        thread_max = fmaxf(thread_max, lane_max);
-        if (a.K) group_max[t * 32 + lane] = lane_max;
+        tile_sums<T, true>(w, a.k, t, lane, blocks, sums, lane_max, bad);
+        if (TOP) {
+            thread_max = fmaxf(thread_max, lane_max);
+            group_max[i * 32 + lane] = lane_max;
+        }
     }
-    __syncthreads();
     if (bad) status |= RSD_ST_NAN_INPUT;
-    if (warp == 0) {
-        const RowTotals t = join(sm.sums, n_tiles, a.k, lane);
-        if (lane == 0) sm.total = t;
+    if (status) tiles::or_at(&status_of_row, 0, status);
+    if constexpr (TOP) block_bound(top_store, thread_max, a.K, rank, blocks);
+    tiles::row_barrier(blocks);
+    if (rank == 0 && warp == 0) {
+        const RowTotals t = join(sums, n_tiles, a.k, lane);
+        if (lane == 0) total_of_row = t;
     }
-    if (there && a.K) top_entries<T, ALIGNED>(a, row, view, n_tiles, thread_max, group_max, top);
-    else __syncthreads();
-    const RowTotals total = sm.total;
+    if constexpr (TOP) {
+        gather_top<T, ALIGNED>(a, view, there ? (n_tiles - (int)rank + (int)blocks - 1) / (int)blocks * 32 : 0, (int)rank, (int)blocks, group_max, top_store, blocks);
+        tiles::row_barrier(blocks);
+    }
+    if (rank != 0) {
+        grid_started();
+        return;
+    }
+    if constexpr (TOP) {
+        if (top_store.overflow || top_store.all_count > kList) top_one_by_one<T>(row, a.V, a.K, top_store);
+    } else {
+        __syncthreads();
+    }
+    const RowTotals total = total_of_row;
     const bool none = !there || total.m == kNegInf;
     const float lnz = none ? 0.0f : logf(total.s);
-    if (there && none) status |= RSD_ST_EMPTY_ROW;
     auto logprob = [&](float v) { return v == kNegInf ? kNegInf : (v - total.m) / a.temp - lnz; };
     if (tid < a.T) {
         if (a.out_logprob) a.out_logprob[slot * a.T + tid] = there && token >= 0 ? logprob(value) : 0.0f;
         if (a.out_token) a.out_token[slot] = there ? token : -1;
     }
-    if (tid == 0 && a.out_entropy) a.out_entropy[slot] = none ? 0.0f : fmaxf(lnz - 0.69314718f * (total.w / total.s), 0.0f);
-    if (a.K) {
-        const int n = there ? min(top.count, kList) : 0;
+    bool few = false;
+    if constexpr (TOP) {
+        const TopSmem& top = top_store;
+        const int n = there ? top.all_count : 0;
+        few = there && n < a.K;
         for (int i = tid; i < n; i += kThreads) {
-            const float v = top.value[i];
-            const int x = top.token[i];
-            int rank = 0;
-            for (int j = 0; j < n; ++j) rank += top.value[j] > v || (top.value[j] == v && top.token[j] < x);
-            if (rank < a.K) {
-                a.out_top_token[slot * a.K + rank] = x;
-                a.out_top_logprob[slot * a.K + rank] = logprob(v);
+            const float v = top.all_value[i];
+            const int x = top.all_token[i];
+            int place = 0;
+            for (int j = 0; j < n; ++j) place += top.all_value[j] > v || (top.all_value[j] == v && top.all_token[j] < x);
+            if (place < a.K) {
+                a.out_top_token[slot * a.K + place] = x;
+                a.out_top_logprob[slot * a.K + place] = logprob(v);
             }
         }
-        if (there && n < a.K) status |= RSD_ST_FEWER_THAN_K;
         for (int i = n + tid; i < a.K; i += kThreads) a.out_top_token[slot * a.K + i] = -1, a.out_top_logprob[slot * a.K + i] = kNegInf;
     }
-    if (status) atomicOr(&sm.status, status);
-    __syncthreads();
-    grid_started();
-    if (!a.own_status) grid_wait();
     if (tid == 0) {
-        if (a.own_status) a.status[b] = sm.status;
-        else if (sm.status) atomicOr(&a.status[b], sm.status);
+        if (a.out_entropy) a.out_entropy[slot] = none ? 0.0f : fmaxf(lnz - 0.69314718f * (total.w / total.s), 0.0f);
+        a.status[slot] = status_of_row | (there && none ? RSD_ST_EMPTY_ROW : 0) | (few ? RSD_ST_FEWER_THAN_K : 0);
     }
+    grid_started();
 }
 
 // d / dv_x of  sum_t g_t log p(token_t) + h H  =  ( sum_{t: token_t = x} g_t - p_x (G + h (log p_x + H)) ) / T,   G = sum_t g_t.
 // The row is read twice, the second time from L2; words of the gradient are written on their own 16-byte boundaries.
 template <typename T, bool ALIGNED, bool ENTROPY>
-__global__ void __launch_bounds__(kThreads) score_grad_kernel(const __grid_constant__ ScoreArgs a) {
+__global__ void __launch_bounds__(kThreads, 3) score_grad_kernel(const __grid_constant__ ScoreArgs a) {
     using P = tiles::Packed16<T>;
     constexpr int E = P::kEntries;
-    __shared__ Smem sm;
+    __shared__ Sums sums;
+    __shared__ RowTotals total_of_row;
+    __shared__ int status_of_row;
     __shared__ int32_t tokens[RSD_MAX_K];
     __shared__ float weights[RSD_MAX_K];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    if (a.own_status) grid_wait();
-    const int64_t slot = blockIdx.x, b = slot / a.R;
+    const uint32_t rank = tiles::cluster_rank(), blocks = tiles::cluster_blocks();
+    if (tid == 0) status_of_row = 0;
+    if (blocks > 1) tiles::cluster_arrive();
+    grid_wait();
+    const int64_t slot = blockIdx.x / blocks, b = slot / a.R;
     const int r = (int)(slot - b * a.R);
     const char* row = (const char*)a.data + (b * a.seq_stride + r * a.row_stride) * (int64_t)sizeof(T);
     char* grad = (char*)a.grad + slot * a.V * (int64_t)sizeof(T);
@@ -321,78 +359,93 @@ __global__ void __launch_bounds__(kThreads) score_grad_kernel(const __grid_const
     }
     const float h = ENTROPY ? a.g_entropy[slot] : 0.0f;
     const tiles::View view = tiles::view_of<T>(row, a.V);
-    const int n_tiles = tiles::tiles_of<T>(a.V, kWords);
-    if (tid == 0) sm.status = 0;
+    const int n_tiles = tiles::tiles_of<T>(a.V, kWords), first = warp * (int)blocks + (int)rank, step = kWarps * (int)blocks;
+    if (blocks > 1) tiles::cluster_wait();
+    else __syncthreads();
     bool bad = false;
-    for (int t = warp; t < n_tiles; t += kWarps) {
+    for (int t = first; t < n_tiles; t += step) {
         uint4 w[kWords];
         tiles::load_tile<T, ALIGNED, kWords>(w, view, t, lane, a.V);
         float lane_max;
-        tile_sums<T, ENTROPY>(w, a.k, t, lane, sm.sums, lane_max, bad);
+        tile_sums<T, ENTROPY>(w, a.k, t, lane, blocks, sums, lane_max, bad);
     }
-    if (__syncthreads_or(bad)) bad = true;
     if (bad) status |= RSD_ST_NAN_INPUT;
+    if (status)
+        for (uint32_t i = 0; i < blocks; ++i) tiles::or_at(&status_of_row, i, status);
+    tiles::row_barrier(blocks);
     if (warp == 0) {
-        const RowTotals t = join(sm.sums, n_tiles, a.k, lane);
-        if (lane == 0) sm.total = t;
+        const RowTotals t = join(sums, n_tiles, a.k, lane);
+        if (lane == 0) total_of_row = t;
     }
     __syncthreads();
-    const RowTotals total = sm.total;
-    const bool none = total.m == kNegInf;
-    if (none) status |= RSD_ST_EMPTY_ROW;
+    const RowTotals total = total_of_row;
+    bad = status_of_row & RSD_ST_NAN_INPUT;
+    const bool none = total.m == kNegInf, plain = tiles::plain_tile(total.m, a.k);
     float G = 0.0f;
     for (int t = 0; t < a.T; ++t) G += weights[t];
-    const float log2z = none ? 0.0f : log2f(total.s), inv_temp = fminf(1.0f / a.temp, 3.0e38f);
+    const float inv_temp = fminf(1.0f / a.temp, 3.0e38f), log2s = none ? 0.0f : log2f(total.s);
+    const float H = ENTROPY && !none ? 0.69314718f * (log2s - total.w / total.s) : 0.0f;
+    // log2 p = v k - c + off, where off is what c = m k + log2 S loses when it is rounded; p and the factor that it is multiplied by take it in
+    const double exact = plain ? (double)total.m * (double)a.k + (double)log2s : (double)log2s;
+    const float c = (float)exact, off = (float)((double)c - exact), scale = exp2f(off);
     // gradient of an entry without a token: p (c0 + c1 log2 p)
-    const float H = ENTROPY && !none ? 0.69314718f * (log2z - total.w / total.s) : 0.0f;
-    const float c0 = none ? 0.0f : -(G + h * H) * inv_temp, c1 = none ? 0.0f : -h * 0.69314718f * inv_temp;
-    const unsigned long long minus_m = tiles::both(none ? 0.0f : -total.m), kk = tiles::both(a.k), minus_l = tiles::both(-log2z), cc0 = tiles::both(c0), cc1 = tiles::both(c1);
-    auto slope = [&](unsigned long long v) {
+    float c1 = none ? 0.0f : -h * 0.69314718f * inv_temp, c0 = none ? 0.0f : fmaf(c1, off, -(G + h * H) * inv_temp);
+    c1 *= scale, c0 *= scale;
+    const unsigned long long minus_m = tiles::both(none || plain ? 0.0f : -total.m), kk = tiles::both(a.k), minus_c = tiles::both(-c), cc0 = tiles::both(c0), cc1 = tiles::both(c1);
+    auto slope = [&](unsigned long long v, auto plain_row) {
         float x, y;
-        split_f32x2(fma_f32x2(add_f32x2(v, minus_m), kk, minus_l), x, y);
-        if (ENTROPY) x = fmaxf(x, tiles::kFarBelow), y = fmaxf(y, tiles::kFarBelow);
+        const unsigned long long l = fma_f32x2(decltype(plain_row)::value ? v : add_f32x2(v, minus_m), kk, minus_c);
+        split_f32x2(l, x, y);
+        if (ENTROPY && !decltype(plain_row)::value) x = fmaxf(x, tiles::kFarBelow), y = fmaxf(y, tiles::kFarBelow);
         const unsigned long long p = f32x2(ex2_approx(x), ex2_approx(y));
         return tiles::mul_f32x2(p, ENTROPY ? fma_f32x2(f32x2(x, y), cc1, cc0) : cc0);
     };
     const int head = (int)((uintptr_t)grad & 15u) / (int)sizeof(T);   // entries between the boundary and the gradient's first one
-    const int words = (head + a.V + E - 1) / E;
-    for (int j = tid; j < words; j += kThreads) {
-        const int x0 = j * E - head;
-        uint4 w = tiles::load_word<T, ALIGNED>(view, x0, a.V);
-        if (bad) {
-            bool ignored = false;
-            P::clean(w, ignored);
+    const int out_tiles = tiles::tiles_of<T>(head + a.V, kWords);
+    auto write = [&](auto plain_row) {
+        for (int t = first; t < out_tiles; t += step) {
+            const int x0 = t * tiles::tile_entries<T>(kWords) + lane * E - head, from = x0 - lane * E;
+            const bool whole = from >= 0 && from + tiles::tile_entries<T>(kWords) <= a.V;
+            uint4 w[kWords];
+            tiles::load_words<T, ALIGNED, kWords>(w, view, x0, whole, a.V);
+#pragma unroll
+            for (int k = 0; k < kWords; ++k) {
+                if (bad) {
+                    bool ignored = false;
+                    P::clean(w[k], ignored);
+                }
+                if (ENTROPY && decltype(plain_row)::value) w[k] = P::raised(w[k]);
+                const uint4 g = P::make([&](int i) { return slope(P::pair(w[k], i), plain_row); });
+                const int x = x0 + k * 32 * E;
+                if (whole || (x >= 0 && x + E <= a.V)) {
+                    *(uint4*)(grad + (int64_t)x * (int)sizeof(T)) = g;
+                } else {
+                    for (int i = 0; i < E; ++i)
+                        if (x + i >= 0 && x + i < a.V) P::store(grad, x + i, P::get(g, i));
+                }
+            }
         }
-        const uint4 g = P::make([&](int i) { return slope(P::pair(w, i)); });
-        if (x0 >= 0 && x0 + E <= a.V) {
-            *(uint4*)(grad + (int64_t)x0 * (int)sizeof(T)) = g;
-        } else {
-            for (int i = 0; i < E; ++i)
-                if (x0 + i >= 0 && x0 + i < a.V) P::store(grad, x0 + i, P::get(g, i));
-        }
-    }
+    };
+    if (plain) write(std::true_type());
+    else write(std::false_type());
     __syncthreads();
-    if (tid < a.T && tokens[tid] >= 0) {       // the tokens' entries again, with their own weights; a token given twice has both
+    // The tokens' entries again, with their own weights, by the block that wrote them; a token given twice has both.
+    if (tid < a.T && tokens[tid] >= 0 && (uint32_t)((tokens[tid] + head) / tiles::tile_entries<T>(kWords)) % blocks == rank) {
         const int32_t x = tokens[tid];
         float own = 0.0f;
-        bool first = true;
+        bool first_of_it = true;
         for (int t = 0; t < a.T; ++t)
-            if (tokens[t] == x) own += weights[t], first = first && t >= tid;
-        if (first) {
+            if (tokens[t] == x) own += weights[t], first_of_it = first_of_it && t >= tid;
+        if (first_of_it) {
             const float v = entry<T>(row, x);
             float rest, ignored;
-            split_f32x2(slope(tiles::both(v)), rest, ignored);
+            if (plain) split_f32x2(slope(tiles::both(fmaxf(v, tiles::kLow)), std::true_type()), rest, ignored);
+            else split_f32x2(slope(tiles::both(v), std::false_type()), rest, ignored);
             P::store(grad, x, none ? 0.0f : fmaf(own, inv_temp, rest));
         }
     }
-    if (status) atomicOr(&sm.status, status);
-    __syncthreads();
+    if (rank == 0 && tid == 0) a.status[slot] = status_of_row | (none ? RSD_ST_EMPTY_ROW : 0);
     grid_started();
-    if (!a.own_status) grid_wait();
-    if (tid == 0) {
-        if (a.own_status) a.status[b] = sm.status;
-        else if (sm.status) atomicOr(&a.status[b], sm.status);
-    }
 }
 
 }  // namespace score

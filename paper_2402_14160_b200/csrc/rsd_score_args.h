@@ -16,7 +16,6 @@ struct ScoreArgs {
     float temp, k;                 // temperature, log2(e) / temperature
     float *out_logprob, *out_entropy, *out_top_logprob;
     int32_t *out_token, *out_top_token, *status;
-    int own_status;                // a sequence of one row: its block stores the status; otherwise it is OR-ed into cleared words
     // gradient
     const float *g_logprob, *g_entropy;
     void* grad;
@@ -30,12 +29,11 @@ struct DivergenceArgs {
     float draft_temp;
     float *out_kl, *out_reverse, *out_overlap;
     int32_t* status;
-    int own_status;
     const float *g_kl, *g_reverse;
     void* grad;
 };
 
-// `slots` rows (or pairs of rows), a block each.  aligned: rows (and gradient rows) start on 16-byte boundaries.
+// `slots` rows (or pairs of rows), a block or a cluster of blocks each.  aligned: rows (and gradient rows) start on 16-byte boundaries.
 void launch_score_f32(bool aligned, unsigned slots, const ScoreArgs& a, cudaStream_t s);
 void launch_score_bf16(bool aligned, unsigned slots, const ScoreArgs& a, cudaStream_t s);
 void launch_score_grad_f32(bool aligned, unsigned slots, const ScoreArgs& a, cudaStream_t s);

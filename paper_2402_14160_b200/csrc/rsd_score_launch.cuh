@@ -8,25 +8,42 @@
 
 namespace rsd {
 
+// Blocks that share a row: few rows leave most of the chip idle, so that their tiles are dealt to the blocks of a cluster.
+inline int row_blocks(unsigned slots, int n_tiles, int warps) {
+    const int sms = rsd_host::sm_count();
+    int blocks = 1;
+    while (blocks < tiles::kMaxBlocks && (int64_t)slots * blocks * 2 <= 2 * sms && n_tiles > blocks * warps) blocks *= 2;
+    return blocks;
+}
+template <typename A>
+void launch_rows(void (*kernel)(A), unsigned slots, int blocks, int threads, size_t smem, cudaStream_t s, const A& a) {
+    rsd_host::launch_overlapped(kernel, slots * (unsigned)blocks, (unsigned)threads, smem, s, blocks > 1 ? blocks : 0, a);
+}
+
 template <typename T>
 void launch_score_of(bool aligned, unsigned slots, const ScoreArgs& a, cudaStream_t s) {
-    const size_t smem = a.K ? (size_t)tiles::tiles_of<T>(a.V, score::kWords) * 32 * sizeof(float) : 0;
-    rsd_host::launch_overlapped(aligned ? score::score_rows_kernel<T, true> : score::score_rows_kernel<T, false>, slots, score::kThreads, smem, s, 0, a);
+    const int n_tiles = tiles::tiles_of<T>(a.V, score::kWords), blocks = row_blocks(slots, n_tiles, score::kWarps);
+    if (a.K) launch_rows(aligned ? score::score_rows_kernel<T, true, true> : score::score_rows_kernel<T, false, true>, slots, blocks, score::kThreads,
+                         (size_t)((n_tiles + blocks - 1) / blocks) * 32 * sizeof(float), s, a);
+    else launch_rows(aligned ? score::score_rows_kernel<T, true, false> : score::score_rows_kernel<T, false, false>, slots, blocks, score::kThreads, 0, s, a);
 }
 template <typename T>
 void launch_score_grad_of(bool aligned, unsigned slots, const ScoreArgs& a, cudaStream_t s) {
-    if (a.g_entropy) rsd_host::launch_overlapped(aligned ? score::score_grad_kernel<T, true, true> : score::score_grad_kernel<T, false, true>, slots, score::kThreads, 0, s, 0, a);
-    else rsd_host::launch_overlapped(aligned ? score::score_grad_kernel<T, true, false> : score::score_grad_kernel<T, false, false>, slots, score::kThreads, 0, s, 0, a);
+    const int blocks = row_blocks(slots, tiles::tiles_of<T>(a.V, score::kWords), score::kWarps);
+    if (a.g_entropy) launch_rows(aligned ? score::score_grad_kernel<T, true, true> : score::score_grad_kernel<T, false, true>, slots, blocks, score::kThreads, 0, s, a);
+    else launch_rows(aligned ? score::score_grad_kernel<T, true, false> : score::score_grad_kernel<T, false, false>, slots, blocks, score::kThreads, 0, s, a);
 }
 template <typename T>
 void launch_divergence_of(bool aligned, unsigned slots, const DivergenceArgs& a, cudaStream_t s) {
-    rsd_host::launch_overlapped(aligned ? divergence::divergence_kernel<T, true> : divergence::divergence_kernel<T, false>, slots, divergence::kThreads, 0, s, 0, a);
+    const int blocks = row_blocks(slots, tiles::tiles_of<T>(a.V, divergence::kWords), divergence::kWarps);
+    launch_rows(aligned ? divergence::divergence_kernel<T, true> : divergence::divergence_kernel<T, false>, slots, blocks, divergence::kThreads, 0, s, a);
 }
 template <typename T>
 void launch_divergence_grad_of(bool aligned, unsigned slots, const DivergenceArgs& a, cudaStream_t s) {
     namespace d = divergence;
-    if (a.g_reverse) rsd_host::launch_overlapped(aligned ? d::divergence_grad_kernel<T, true, true> : d::divergence_grad_kernel<T, false, true>, slots, d::kThreads, 0, s, 0, a);
-    else rsd_host::launch_overlapped(aligned ? d::divergence_grad_kernel<T, true, false> : d::divergence_grad_kernel<T, false, false>, slots, d::kThreads, 0, s, 0, a);
+    const int blocks = row_blocks(slots, tiles::tiles_of<T>(a.V, d::kWords), d::kWarps);
+    if (a.g_reverse) launch_rows(aligned ? d::divergence_grad_kernel<T, true, true> : d::divergence_grad_kernel<T, false, true>, slots, blocks, d::kThreads, 0, s, a);
+    else launch_rows(aligned ? d::divergence_grad_kernel<T, true, false> : d::divergence_grad_kernel<T, false, false>, slots, blocks, d::kThreads, 0, s, a);
 }
 
 }  // namespace rsd

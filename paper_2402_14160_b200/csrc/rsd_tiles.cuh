@@ -5,6 +5,8 @@
 // are joined in the order of the tiles.  So a row gives the same bits whatever the number of warps or blocks that share it, the rows beside it
 // and the address that it starts at.
 #pragma once
+#include <type_traits>
+
 #include "rsd_device.cuh"
 #include "rsd_scan.cuh"   // ex2_approx, packed arithmetic
 
@@ -24,14 +26,27 @@ __device__ __forceinline__ View view_of(const void* row, int V) {
     return {(const char*)row - first, first, (first + V * (int)sizeof(T) - 1) >> 4};
 }
 
-// bytes shift .. shift + 15 of two adjacent granules
-__device__ __forceinline__ uint4 shifted(const uint4& a, const uint4& b, int shift) {
-    const bool one = shift & 4, two = shift & 8;
-    const uint32_t x0 = one ? a.y : a.x, x1 = one ? a.z : a.y, x2 = one ? a.w : a.z, x3 = one ? b.x : a.w, x4 = one ? b.y : b.x, x5 = one ? b.z : b.y, x6 = one ? b.w : b.z;
-    const uint32_t y0 = two ? x2 : x0, y1 = two ? x3 : x1, y2 = two ? x4 : x2, y3 = two ? x5 : x3, y4 = two ? x6 : x4;
-    const int bits = (shift & 3) * 8;
-    return make_uint4(__funnelshift_r(y0, y1, bits), __funnelshift_r(y1, y2, bits), __funnelshift_r(y2, y3, bits), __funnelshift_r(y3, y4, bits));
+// bytes shift .. shift + 15 of two adjacent granules, shift = 4 Q + bits / 8
+template <int Q>
+__device__ __forceinline__ uint4 shifted(const uint4& a, const uint4& b, int bits) {
+    const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    return make_uint4(__funnelshift_r(w[Q], w[Q + 1], bits), __funnelshift_r(w[Q + 1], w[Q + 2], bits), __funnelshift_r(w[Q + 2], w[Q + 3], bits),
+                      __funnelshift_r(w[Q + 3], w[(Q + 4) & 7], bits));
 }
+// f(Q) for a shift that is the same for all threads
+template <typename F>
+__device__ __forceinline__ void with_shift(int shift, F f) {
+    switch (shift >> 2) {
+        case 0: f(std::integral_constant<int, 0>()); break;
+        case 1: f(std::integral_constant<int, 1>()); break;
+        case 2: f(std::integral_constant<int, 2>()); break;
+        default: f(std::integral_constant<int, 3>()); break;
+    }
+}
+
+// Entries are raised to this where 0 times -inf would not be a number: their weight stays 0.  Plain arithmetic holds where a tile's largest entry is far above it
+// and the exponents' scale keeps it finite.
+constexpr float kLow = -1e30f, kPlainEntry = 1e28f, kPlainScale = 1e6f;
 
 template <typename T>
 struct Packed16;   // one word as entries
@@ -58,17 +73,28 @@ struct Packed16<float> {
     }
     __device__ static __forceinline__ uint4 masked() { return make_uint4(kMasked, kMasked, kMasked, kMasked); }
     template <int KW>
-    __device__ static __forceinline__ void bounds(const uint4 (&w)[KW], float& mx, float& mn) {   // mx: NaN if there is one
-        float a = __uint_as_float(w[0].x), b = a;
+    __device__ static __forceinline__ float largest(const uint4 (&w)[KW]) {   // NaN if there is one
+        float a = max_nan(__uint_as_float(w[0].x), __uint_as_float(w[0].y));
+        a = max_nan(a, max_nan(__uint_as_float(w[0].z), __uint_as_float(w[0].w)));
 #pragma unroll
-        for (int k = 0; k < KW; ++k) {
-            const float p = max_nan(__uint_as_float(w[k].x), __uint_as_float(w[k].y)), q = max_nan(__uint_as_float(w[k].z), __uint_as_float(w[k].w));
-            a = max_nan(a, max_nan(p, q));
-            const float r = fminf(__uint_as_float(w[k].x), __uint_as_float(w[k].y)), s = fminf(__uint_as_float(w[k].z), __uint_as_float(w[k].w));
-            b = fminf(b, fminf(r, s));
-        }
-        mx = a, mn = b;
+        for (int k = 1; k < KW; ++k)
+            a = max_nan(a, max_nan(max_nan(__uint_as_float(w[k].x), __uint_as_float(w[k].y)), max_nan(__uint_as_float(w[k].z), __uint_as_float(w[k].w))));
+        return a;
     }
+    template <int KW>
+    __device__ static __forceinline__ float smallest(const uint4 (&w)[KW]) {
+        float a = fminf(__uint_as_float(w[0].x), __uint_as_float(w[0].y));
+        a = fminf(a, fminf(__uint_as_float(w[0].z), __uint_as_float(w[0].w)));
+#pragma unroll
+        for (int k = 1; k < KW; ++k)
+            a = fminf(a, fminf(fminf(__uint_as_float(w[k].x), __uint_as_float(w[k].y)), fminf(__uint_as_float(w[k].z), __uint_as_float(w[k].w))));
+        return a;
+    }
+    __device__ static __forceinline__ uint32_t raised_entry(uint32_t u) { return __float_as_uint(fmaxf(__uint_as_float(u), kLow)); }
+    __device__ static __forceinline__ uint4 raised(const uint4& w) { return make_uint4(raised_entry(w.x), raised_entry(w.y), raised_entry(w.z), raised_entry(w.w)); }
+    // whether one of two words has an entry above kLow where the other has none
+    __device__ static __forceinline__ bool differ(uint32_t a, uint32_t b) { return (__uint_as_float(a) > kLow) != (__uint_as_float(b) > kLow); }
+    __device__ static __forceinline__ bool differ(const uint4& a, const uint4& b) { return differ(a.x, b.x) | differ(a.y, b.y) | differ(a.z, b.z) | differ(a.w, b.w); }
     // f(pair of entries) for the pairs of a word
     template <typename F>
     __device__ static __forceinline__ void pairs(const uint4& w, F f) {
@@ -122,15 +148,33 @@ struct Packed16<__nv_bfloat16> {
         return r;
     }
     template <int KW>
-    __device__ static __forceinline__ void bounds(const uint4 (&w)[KW], float& mx, float& mn) {
-        uint32_t a = w[0].x, b = w[0].x;
+    __device__ static __forceinline__ float largest(const uint4 (&w)[KW]) {
+        uint32_t a = bf162_max_nan(bf162_max_nan(w[0].x, w[0].y), bf162_max_nan(w[0].z, w[0].w));
 #pragma unroll
-        for (int k = 0; k < KW; ++k) {
-            a = bf162_max_nan(a, bf162_max_nan(bf162_max_nan(w[k].x, w[k].y), bf162_max_nan(w[k].z, w[k].w)));
-            b = min2(b, min2(min2(w[k].x, w[k].y), min2(w[k].z, w[k].w)));
-        }
-        mx = max_nan(__uint_as_float(a << 16), __uint_as_float(a & 0xFFFF0000u));
-        mn = fminf(__uint_as_float(b << 16), __uint_as_float(b & 0xFFFF0000u));
+        for (int k = 1; k < KW; ++k) a = bf162_max_nan(a, bf162_max_nan(bf162_max_nan(w[k].x, w[k].y), bf162_max_nan(w[k].z, w[k].w)));
+        return max_nan(__uint_as_float(a << 16), __uint_as_float(a & 0xFFFF0000u));
+    }
+    template <int KW>
+    __device__ static __forceinline__ float smallest(const uint4 (&w)[KW]) {
+        uint32_t a = min2(min2(w[0].x, w[0].y), min2(w[0].z, w[0].w));
+#pragma unroll
+        for (int k = 1; k < KW; ++k) a = min2(a, min2(min2(w[k].x, w[k].y), min2(w[k].z, w[k].w)));
+        return fminf(__uint_as_float(a << 16), __uint_as_float(a & 0xFFFF0000u));
+    }
+    static constexpr uint32_t kLow2 = 0xF149F149u;   // kLow rounded to this type, twice
+    __device__ static __forceinline__ uint32_t raised_entry(uint32_t u) {
+        uint32_t r;
+        asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(u), "r"(kLow2));
+        return r;
+    }
+    __device__ static __forceinline__ uint4 raised(const uint4& w) { return make_uint4(raised_entry(w.x), raised_entry(w.y), raised_entry(w.z), raised_entry(w.w)); }
+    __device__ static __forceinline__ uint32_t none(uint32_t u) {   // 0xFFFF per half without an entry above kLow
+        uint32_t r;
+        asm("set.le.u32.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(u), "r"(kLow2));
+        return r;
+    }
+    __device__ static __forceinline__ bool differ(const uint4& a, const uint4& b) {
+        return ((none(a.x) ^ none(b.x)) | (none(a.y) ^ none(b.y)) | (none(a.z) ^ none(b.z)) | (none(a.w) ^ none(b.w))) != 0;
     }
     __device__ static __forceinline__ unsigned long long unpack(uint32_t u) { return f32x2(__uint_as_float(u << 16), __uint_as_float(u & 0xFFFF0000u)); }
     template <typename F>
@@ -176,16 +220,74 @@ __device__ __forceinline__ uint4 load_word(const View& v, int x0, int V) {
         uint4 b = w;
         if (g >= 0) w = ld_shared_word(v.base + (int64_t)g * 16);
         if (g < v.last) b = ld_shared_word(v.base + (int64_t)(g + 1) * 16);
-        w = shifted(w, b, shift);
+        with_shift(shift, [&](auto q) { w = shifted<decltype(q)::value>(w, b, (shift & 3) * 8); });
     }
     if (x0 < 0 || x0 + E > V) Packed16<T>::keep(w, -x0, V - x0);
     return w;
 }
 
+// KW words of a lane, 32 words apart, from entry x0 on
+template <typename T, bool ALIGNED, int KW>
+__device__ __forceinline__ void load_words(uint4 (&w)[KW], const View& v, int x0, bool whole, int V) {   // whole: every word of the warp lies in the row
+    constexpr int E = Packed16<T>::kEntries;
+    if (whole) {
+        const int at = v.first + x0 * (int)sizeof(T), shift = at & 15;
+        const char* p = v.base + (at & ~15);
+        if (ALIGNED || shift == 0) {
+#pragma unroll
+            for (int k = 0; k < KW; ++k) w[k] = ld_stream(p + k * 512);
+        } else {                                   // (the word's last entry lies in the second granule)
+            with_shift(shift, [&](auto q) {
+#pragma unroll
+                for (int k = 0; k < KW; ++k) w[k] = shifted<decltype(q)::value>(ld_shared_word(p + k * 512), ld_shared_word(p + k * 512 + 16), (shift & 3) * 8);
+            });
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < KW; ++k) w[k] = load_word<T, ALIGNED>(v, x0 + k * 32 * E, V);
+    }
+}
 template <typename T, bool ALIGNED, int KW>
 __device__ __forceinline__ void load_tile(uint4 (&w)[KW], const View& v, int t, int lane, int V) {
-#pragma unroll
-    for (int k = 0; k < KW; ++k) w[k] = load_word<T, ALIGNED>(v, ((t * KW + k) * 32 + lane) * Packed16<T>::kEntries, V);
+    load_words<T, ALIGNED, KW>(w, v, t * tile_entries<T>(KW) + lane * Packed16<T>::kEntries, (t + 1) * tile_entries<T>(KW) <= V, V);
+}
+
+// ---- a row's blocks: one, or a cluster of up to eight that deal out its tiles -----------------------------------------------------------------
+constexpr int kMaxBlocks = 8;
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ uint32_t cluster_blocks() {
+    uint32_t r;
+    asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ uint32_t remote(const void* p, uint32_t rank) {   // the same place in another block's shared memory
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_u32(p)), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ void store_at(float* p, uint32_t rank, float v) { asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(remote(p, rank)), "f"(v) : "memory"); }
+__device__ __forceinline__ void store_at(int* p, uint32_t rank, int v) { asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(remote(p, rank)), "r"(v) : "memory"); }
+__device__ __forceinline__ void or_at(int* p, uint32_t rank, int v) { asm volatile("red.shared::cluster.or.b32 [%0], %1;" ::"r"(remote(p, rank)), "r"(v) : "memory"); }
+__device__ __forceinline__ void max_at(uint32_t* p, uint32_t rank, uint32_t v) { asm volatile("red.shared::cluster.max.u32 [%0], %1;" ::"r"(remote(p, rank)), "r"(v) : "memory"); }
+__device__ __forceinline__ int add_at(int* p, uint32_t rank, int v) {
+    int r;
+    asm volatile("atom.shared::cluster.add.u32 %0, [%1], %2;" : "=r"(r) : "r"(remote(p, rank)), "r"(v) : "memory");
+    return r;
+}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+// Every thread of the row's blocks; what they wrote before is visible behind it.
+__device__ __forceinline__ void row_barrier(uint32_t blocks) {
+    if (blocks > 1) {
+        cluster_arrive();
+        cluster_wait();
+    } else {
+        __syncthreads();
+    }
 }
 
 __device__ __forceinline__ float warp_max_nan(float v) {   // NaN if any lane has one
@@ -217,8 +319,12 @@ __device__ __forceinline__ float warp_sum_four(float a, float b, float c, float 
     return mine;
 }
 
-// Exponents below this give weights of 0 and may be replaced by it: 0 times it is 0, where 0 times -inf is not a number.
+// Exponents below this give weights of 0 and may be replaced by it.
 constexpr float kFarBelow = -1e30f;
+
+// What m k loses when it is rounded: plain tiles take their weights relative to the rounded m k, the others to m k itself.
+__device__ __forceinline__ bool plain_tile(float m, float k) { return fabsf(m) < kPlainEntry && k < kPlainScale; }
+__device__ __forceinline__ float rounded_off(float m, float k) { return plain_tile(m, k) ? fmaf(m, k, -(m * k)) : 0.0f; }
 
 }  // namespace tiles
 }  // namespace rsd
