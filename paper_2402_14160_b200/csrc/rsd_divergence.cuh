@@ -178,9 +178,10 @@ template <typename T>
 __device__ __forceinline__ Pair pair_of(const DivergenceArgs& a) {
     Pair w;
     w.rank = tiles::cluster_rank(), w.blocks = tiles::cluster_blocks();
-    w.slot = blockIdx.x / w.blocks;
-    const int64_t b = w.slot / a.R;
-    const int r = (int)(w.slot - b * a.R);
+    const uint32_t slot = blockIdx.x / w.blocks, sequence = slot / (uint32_t)a.R;
+    const int64_t b = sequence;
+    const int r = (int)(slot - sequence * (uint32_t)a.R);
+    w.slot = slot;
     w.draft = tiles::view_of<T>((const T*)a.draft + b * a.draft_seq + r * a.draft_row, a.V);
     w.target = tiles::view_of<T>((const T*)a.target + b * a.target_seq + r * a.target_row, a.V);
     w.n_tiles = tiles::tiles_of<T>(a.V, kWords);

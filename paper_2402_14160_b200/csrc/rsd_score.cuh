@@ -12,37 +12,43 @@ namespace rsd {
 
 namespace score {
 
-constexpr int kThreads = 256, kWarps = kThreads / 32, kWords = 8;
-constexpr int kMaxTiles = RSD_MAX_VOCAB / tiles::tile_entries<float>(kWords);
-constexpr int kBuckets = 64;       // samples that bound the K-th largest entry; at least RSD_MAX_K
+constexpr int kWords = 8;
+constexpr int kBuckets = 64;       // samples that bound the K-th largest entry: two per lane
 constexpr int kList = 512;         // groups opened, and entries taken from them
-static_assert(kBuckets == 64 && kBuckets >= RSD_MAX_K, "two buckets per lane");
+static_assert(kBuckets >= RSD_MAX_K, "");
 
-struct Sums {                      // of a row's tiles, relative to each tile's largest entry; every block of the row has all of them
-    float m[kMaxTiles], s[kMaxTiles], w[kMaxTiles];
+struct Sums {                      // of a row's n tiles, relative to each tile's largest entry; every block of the row has all of them
+    float *m, *s, *w;
+    __device__ __forceinline__ Sums(float* at, int n) : m(at), s(at + n), w(at + 2 * n) {}
 };
+inline size_t sums_bytes(int n) { return (size_t)n * 3 * sizeof(float); }
 struct RowTotals {
     float m, s, w;                 // largest entry; sum of 2^y, of 2^y y
 };
 
-// Sum of 2^y and of 2^y y over a tile, y = (v - m) k, to all blocks of the row; lane_max: the lane's largest entry.
-template <typename T, bool ENTROPY>
-__device__ __forceinline__ void tile_sums(uint4 (&w)[kWords], float k, int t, int lane, uint32_t blocks, Sums& sums, float& lane_max, bool& bad) {
+// Sum of 2^y and of 2^y y over a tile, y = (v - m) k, to all blocks of the row; lane_max: the lane's largest entry.  refill(i) reads word i of
+// the warp's next tile into its place as soon as it is free, so that half of the work and the sums over the warp go on while the words are on their way.
+template <typename T, bool ENTROPY, typename F>
+__device__ __forceinline__ void tile_sums(uint4 (&w)[kWords], float k, int t, int lane, uint32_t blocks, const Sums& sums, float& lane_max, bool& bad, F refill) {
     using P = tiles::Packed16<T>;
     float mx = P::largest(w), m = tiles::warp_max_nan(mx);
     unsigned long long s = tiles::both(0.0f), e = s;
     if (tiles::plain_tile(m, k)) {
         const unsigned long long ref = tiles::both(-(m * k)), kk = tiles::both(k);
 #pragma unroll
-        for (int i = 0; i < kWords; ++i)
-            P::pairs(ENTROPY ? P::raised(w[i]) : w[i], [&](unsigned long long v) {
-                const unsigned long long y = fma_f32x2(v, kk, ref);
-                float a, b;
-                split_f32x2(y, a, b);
-                const unsigned long long x = f32x2(ex2_approx(a), ex2_approx(b));
-                s = add_f32x2(s, x);
-                if (ENTROPY) e = fma_f32x2(x, y, e);
-            });
+        for (int half = 0; half < kWords; half += kWords / 2) {
+#pragma unroll
+            for (int i = half; i < half + kWords / 2; ++i)
+                P::pairs(ENTROPY ? P::raised(w[i]) : w[i], [&](unsigned long long v) {
+                    const unsigned long long y = fma_f32x2(v, kk, ref);
+                    float a, b;
+                    split_f32x2(y, a, b);
+                    const unsigned long long x = f32x2(ex2_approx(a), ex2_approx(b));
+                    s = add_f32x2(s, x);
+                    if (ENTROPY) e = fma_f32x2(x, y, e);
+                });
+            refill(half);
+        }
     } else {                                        // no entry, NaN, +inf, or values or a scale near the end of the range
         if (!(m < __builtin_huge_valf())) {
 #pragma unroll
@@ -63,6 +69,8 @@ __device__ __forceinline__ void tile_sums(uint4 (&w)[kWords], float k, int t, in
                     e = fma_f32x2(x, f32x2(a, b), e);
                 });
         }
+        refill(0);
+        refill(kWords / 2);
     }
     lane_max = mx;
     float s0, s1, e0, e1;
@@ -75,6 +83,18 @@ __device__ __forceinline__ void tile_sums(uint4 (&w)[kWords], float k, int t, in
         else if (lane < 16) tiles::store_at(&sums.m[t], to, m);
         else if (lane < 24) tiles::store_at(&sums.w[t], to, sum);
     }
+}
+
+// Half of the words of a tile; nothing where there is no such tile.
+template <typename T, bool ALIGNED>
+__device__ __forceinline__ void load_half(uint4 (&w)[kWords], const tiles::View& view, int t, int half, int lane, int V) {
+    constexpr int kHalf = kWords / 2, E = tiles::Packed16<T>::kEntries;
+    const int from = t * tiles::tile_entries<T>(kWords) + half * 32 * E;
+    if (t * tiles::tile_entries<T>(kWords) >= V) return;
+    uint4 h[kHalf];
+    tiles::load_words<T, ALIGNED, kHalf>(h, view, from + lane * E, from + tiles::tile_entries<T>(kHalf) <= V, V);
+#pragma unroll
+    for (int i = 0; i < kHalf; ++i) w[half + i] = h[i];
 }
 
 // The tiles' sums joined by one warp; every lane gets the result.
@@ -101,17 +121,20 @@ __device__ __forceinline__ float entry(const void* row, int x) {   // -inf where
 }
 
 // ---- the K largest entries of a row ----------------------------------------------------------------------------------------------
-// Every lane knows its largest entry of each tile (a group of up to 64 entries).  A block's largest entries per thread, taken together into
-// kBuckets buckets, are distinct entries: the K-th largest of them is at most the K-th largest entry of the row, and so is the largest such bound of
-// the row's blocks.  Only groups that reach their block's bound are read again (they lie in L2), a word a thread, and only entries that reach the row's are
+// Every lane knows its largest entry of each tile (a group of up to 64 entries).  The largest of a block's even and of its odd tiles in each lane are
+// kBuckets distinct entries: the K-th largest of them is at most the K-th largest entry of the row, and so is the largest such bound of
+// the row's blocks.  Only groups that reach it are read again (they lie in L2), a word a thread, and only entries that reach it are
 // ranked: about 1.4 K of them.
+template <int NW>
 struct TopSmem {
-    float bucket[kThreads];
+    float bucket[NW][kBuckets];
     float bound[tiles::kMaxBlocks];   // of every block of the row
     int32_t group[kList];
     float all_value[kList];           // in the first block: the entries of all
     int32_t all_token[kList];
     int groups, all_count, overflow;
+    float best_value[NW];
+    int best_token[NW];
 };
 
 // K-th largest of 64 values, two per lane, from below: exact in its upper 16 bits.
@@ -127,16 +150,14 @@ __device__ __forceinline__ float bound_of_kth(float a, float b, int K) {
 }
 
 // Beyond the list: the entries one after the other, each the best below the one before.
-template <typename T>
-__device__ __noinline__ void top_one_by_one(const void* row, int V, int K, TopSmem& sm) {
-    __shared__ float best_v[kWarps];
-    __shared__ int best_x[kWarps];
+template <typename T, int NW>
+__device__ __noinline__ void top_one_by_one(const void* row, int V, int K, TopSmem<NW>& sm) {
     float last_v = __builtin_huge_valf();
     int last_x = -1, found = 0;
     for (; found < K; ++found) {
         float v = kNegInf;
         int at = -1;
-        for (int x = threadIdx.x; x < V; x += kThreads) {
+        for (int x = threadIdx.x; x < V; x += NW * 32) {
             const float u = entry<T>(row, x);
             if (u > v && (u < last_v || (u == last_v && x > last_x))) v = u, at = x;
         }
@@ -147,11 +168,11 @@ __device__ __noinline__ void top_one_by_one(const void* row, int V, int K, TopSm
             if (ox >= 0 && (at < 0 || ov > v || (ov == v && ox < at))) v = ov, at = ox;
         }
         __syncthreads();
-        if ((threadIdx.x & 31) == 0) best_v[threadIdx.x >> 5] = v, best_x[threadIdx.x >> 5] = at;
+        if ((threadIdx.x & 31) == 0) sm.best_value[threadIdx.x >> 5] = v, sm.best_token[threadIdx.x >> 5] = at;
         __syncthreads();
-        v = best_v[0], at = best_x[0];
-        for (int j = 1; j < kWarps; ++j)
-            if (best_x[j] >= 0 && (at < 0 || best_v[j] > v || (best_v[j] == v && best_x[j] < at))) v = best_v[j], at = best_x[j];
+        v = sm.best_value[0], at = sm.best_token[0];
+        for (int j = 1; j < NW; ++j)
+            if (sm.best_token[j] >= 0 && (at < 0 || sm.best_value[j] > v || (sm.best_value[j] == v && sm.best_token[j] < at))) v = sm.best_value[j], at = sm.best_token[j];
         if (at < 0) break;
         last_v = v, last_x = at;
         if (threadIdx.x == 0) sm.all_value[found] = v, sm.all_token[found] = at;
@@ -161,29 +182,30 @@ __device__ __noinline__ void top_one_by_one(const void* row, int V, int K, TopSm
     __syncthreads();
 }
 
-// Bound of a block, known to all blocks of the row behind the next barrier.
-__device__ __forceinline__ void block_bound(TopSmem& sm, float thread_max, int K, uint32_t rank, uint32_t blocks) {
-    const int tid = threadIdx.x;
-    sm.bucket[tid] = thread_max;
-    __syncthreads();
-    if (tid < 32) {
-        float u = kNegInf, v = kNegInf;
-#pragma unroll
-        for (int i = 0; i < kThreads; i += kBuckets) u = fmaxf(u, sm.bucket[i + tid]), v = fmaxf(v, sm.bucket[i + 32 + tid]);
-        const float b = bound_of_kth(u, v, K);
-        if ((uint32_t)tid < blocks) tiles::store_at(&sm.bound[rank], (uint32_t)tid, b);
+// Bound of a block, known to all blocks of the row behind the next barrier.  even, odd: the lane's largest entries.
+template <int NW>
+__device__ __forceinline__ void block_bound(TopSmem<NW>& sm, float even, float odd, int K, uint32_t rank, uint32_t blocks) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    if (NW > 1) {
+        sm.bucket[warp][lane] = even, sm.bucket[warp][lane + 32] = odd;
+        __syncthreads();
+    }
+    if (warp == 0) {
+        for (int i = 1; i < NW; ++i) even = fmaxf(even, sm.bucket[i][lane]), odd = fmaxf(odd, sm.bucket[i][lane + 32]);
+        const float b = bound_of_kth(even, odd, K);
+        if ((uint32_t)lane < blocks) tiles::store_at(&sm.bound[rank], (uint32_t)lane, b);
     }
 }
 
 // The entries of the block's tiles that reach the row's bound, in the first block's list.
-template <typename T, bool ALIGNED>
-__device__ __forceinline__ void gather_top(const ScoreArgs& a, const tiles::View& view, int n_groups, int first_tile, int tile_step, const float* group_max, TopSmem& sm,
+template <typename T, bool ALIGNED, int NW>
+__device__ __forceinline__ void gather_top(const ScoreArgs& a, const tiles::View& view, int n_groups, int first_tile, int tile_step, const float* group_max, TopSmem<NW>& sm,
                                            uint32_t blocks) {
     using P = tiles::Packed16<T>;
     const int tid = threadIdx.x;
     float bound = sm.bound[0];
     for (uint32_t i = 1; i < blocks; ++i) bound = fmaxf(bound, sm.bound[i]);
-    for (int i = tid; i < n_groups; i += kThreads)
+    for (int i = tid; i < n_groups; i += NW * 32)
         if (group_max[i] >= bound && group_max[i] > kNegInf) {
             const int at = atomicAdd(&sm.groups, 1);
             if (at < kList) sm.group[at] = i;
@@ -193,7 +215,7 @@ __device__ __forceinline__ void gather_top(const ScoreArgs& a, const tiles::View
     if (groups > kList) {
         if (tid == 0) tiles::store_at(&sm.overflow, 0, 1);
     } else {
-        for (int i = tid; i < groups * kWords; i += kThreads) {
+        for (int i = tid; i < groups * kWords; i += NW * 32) {
             // group i: lane i & 31 of the block's (i >> 5)-th tile
             const int g = sm.group[i / kWords], t = first_tile + (g >> 5) * tile_step, x0 = ((t * kWords + i % kWords) * 32 + (g & 31)) * P::kEntries;
             const uint4 w = tiles::load_word<T, ALIGNED>(view, x0, a.V);
@@ -217,12 +239,12 @@ __device__ __forceinline__ bool slot_of(const ScoreArgs& a, int64_t slot, int64_
     int64_t at = r;
     bool there = true;
     path_token = -1;
-    row = nullptr;
-    if (a.accepted_len) {
-        const int len = a.accepted_len[b], L = a.R - 1;
-        if (len < 0 || len > L || r > len) return false;
-        if (r > 0) at = a.accepted_node[b * L + r - 1];
-        path_token = r < len ? a.accepted_token[b * L + r] : a.last_token[b];
+    if (a.accepted_len) {                          // (what the slot needs is read before it is known whether the path reaches it)
+        const int L = a.R - 1, len = a.accepted_len[b], node = r > 0 ? a.accepted_node[b * L + r - 1] : 0;
+        path_token = r < L ? a.accepted_token[b * L + r] : -1;
+        const int last = a.last_token[b];
+        if (r >= len) path_token = last;
+        at = len >= 0 && len <= L && r <= len ? node : -1;
     } else if (a.row_index) {
         at = a.row_index[slot];
     }
@@ -232,14 +254,13 @@ __device__ __forceinline__ bool slot_of(const ScoreArgs& a, int64_t slot, int64_
     return there;
 }
 
-// Tiles of a row are dealt to the warps of its blocks in turn: tile t to warp t / blocks mod kWarps of block t mod blocks.
-template <typename T, bool ALIGNED, bool TOP>
-__global__ void __launch_bounds__(kThreads, 3) score_rows_kernel(const __grid_constant__ ScoreArgs a) {
-    extern __shared__ float group_max[];           // [tiles of the block][32] where the largest entries are asked for
-    __shared__ Sums sums;
+// Tiles of a row are dealt to the warps of its blocks in turn: tile t to warp t / blocks mod NW of block t mod blocks.
+template <typename T, bool ALIGNED, bool TOP, int NW>
+__global__ void __launch_bounds__(NW * 32, 32 / NW) score_rows_kernel(const __grid_constant__ ScoreArgs a) {
+    extern __shared__ float dynamic[];             // the tiles' sums, and [tiles of the block][32] largest entries where the likeliest tokens are asked for
     __shared__ RowTotals total_of_row;
     __shared__ int status_of_row;
-    __shared__ typename std::conditional<TOP, TopSmem, int>::type top_store;
+    __shared__ typename std::conditional<TOP, TopSmem<NW>, int>::type top_store;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t rank = tiles::cluster_rank(), blocks = tiles::cluster_blocks();
     if (tid == 0) {
@@ -248,8 +269,9 @@ __global__ void __launch_bounds__(kThreads, 3) score_rows_kernel(const __grid_co
     }
     if (blocks > 1) tiles::cluster_arrive();       // (the row's other blocks have started, and their words above are set, behind the wait below)
     grid_wait();
-    const int64_t slot = blockIdx.x / blocks, b = slot / a.R;
-    const int r = (int)(slot - b * a.R);
+    const uint32_t slot_word = blockIdx.x / blocks, sequence = slot_word / (uint32_t)a.R;
+    const int64_t slot = slot_word, b = sequence;
+    const int r = (int)(slot_word - sequence * (uint32_t)a.R);
     int status = 0;
     int32_t path_token;
     const char* row;
@@ -262,31 +284,37 @@ __global__ void __launch_bounds__(kThreads, 3) score_rows_kernel(const __grid_co
         if (there && token >= 0) value = entry<T>(row, token);
     }
     const tiles::View view = tiles::view_of<T>(row, a.V);
-    const int n_tiles = there ? tiles::tiles_of<T>(a.V, kWords) : 0;
+    const int all_tiles = tiles::tiles_of<T>(a.V, kWords), n_tiles = there ? all_tiles : 0;
+    const Sums sums(dynamic, all_tiles);
+    float* const group_max = dynamic + 3 * all_tiles;
+    uint4 w[kWords];
+    const int step = NW * (int)blocks;
+    int t = warp * (int)blocks + (int)rank;
+    load_half<T, ALIGNED>(w, view, t, 0, lane, there ? a.V : 0), load_half<T, ALIGNED>(w, view, t, kWords / 2, lane, there ? a.V : 0);
     if (blocks > 1) tiles::cluster_wait();
     else __syncthreads();
-    float thread_max = kNegInf;
+    float even = kNegInf, odd = kNegInf;
     bool bad = false;
-    for (int i = warp, t = warp * (int)blocks + (int)rank; t < n_tiles; i += kWarps, t += kWarps * (int)blocks) {   // i: the tile's place in the block
-        uint4 w[kWords];
-        tiles::load_tile<T, ALIGNED, kWords>(w, view, t, lane, a.V);
+#pragma unroll 1
+    for (int i = warp; t < n_tiles; i += NW, t += step) {   // i: the tile's place in the block
         float lane_max;
-        tile_sums<T, true>(w, a.k, t, lane, blocks, sums, lane_max, bad);
+        tile_sums<T, true>(w, a.k, t, lane, blocks, sums, lane_max, bad, [&](int half) { load_half<T, ALIGNED>(w, view, t + step, half, lane, a.V); });
         if (TOP) {
-            thread_max = fmaxf(thread_max, lane_max);
             group_max[i * 32 + lane] = lane_max;
+            if (i & 1) odd = fmaxf(odd, lane_max);
+            else even = fmaxf(even, lane_max);
         }
     }
     if (bad) status |= RSD_ST_NAN_INPUT;
     if (status) tiles::or_at(&status_of_row, 0, status);
-    if constexpr (TOP) block_bound(top_store, thread_max, a.K, rank, blocks);
+    if constexpr (TOP) block_bound<NW>(top_store, even, odd, a.K, rank, blocks);
     tiles::row_barrier(blocks);
     if (rank == 0 && warp == 0) {
         const RowTotals t = join(sums, n_tiles, a.k, lane);
         if (lane == 0) total_of_row = t;
     }
     if constexpr (TOP) {
-        gather_top<T, ALIGNED>(a, view, there ? (n_tiles - (int)rank + (int)blocks - 1) / (int)blocks * 32 : 0, (int)rank, (int)blocks, group_max, top_store, blocks);
+        gather_top<T, ALIGNED, NW>(a, view, there ? (n_tiles - (int)rank + (int)blocks - 1) / (int)blocks * 32 : 0, (int)rank, (int)blocks, group_max, top_store, blocks);
         tiles::row_barrier(blocks);
     }
     if (rank != 0) {
@@ -294,7 +322,7 @@ __global__ void __launch_bounds__(kThreads, 3) score_rows_kernel(const __grid_co
         return;
     }
     if constexpr (TOP) {
-        if (top_store.overflow || top_store.all_count > kList) top_one_by_one<T>(row, a.V, a.K, top_store);
+        if (top_store.overflow || top_store.all_count > kList) top_one_by_one<T, NW>(row, a.V, a.K, top_store);
     } else {
         __syncthreads();
     }
@@ -308,10 +336,10 @@ __global__ void __launch_bounds__(kThreads, 3) score_rows_kernel(const __grid_co
     }
     bool few = false;
     if constexpr (TOP) {
-        const TopSmem& top = top_store;
+        const TopSmem<NW>& top = top_store;
         const int n = there ? top.all_count : 0;
         few = there && n < a.K;
-        for (int i = tid; i < n; i += kThreads) {
+        for (int i = tid; i < n; i += NW * 32) {
             const float v = top.all_value[i];
             const int x = top.all_token[i];
             int place = 0;
@@ -321,7 +349,7 @@ __global__ void __launch_bounds__(kThreads, 3) score_rows_kernel(const __grid_co
                 a.out_top_logprob[slot * a.K + place] = logprob(v);
             }
         }
-        for (int i = n + tid; i < a.K; i += kThreads) a.out_top_token[slot * a.K + i] = -1, a.out_top_logprob[slot * a.K + i] = kNegInf;
+        for (int i = n + tid; i < a.K; i += NW * 32) a.out_top_token[slot * a.K + i] = -1, a.out_top_logprob[slot * a.K + i] = kNegInf;
     }
     if (tid == 0) {
         if (a.out_entropy) a.out_entropy[slot] = none ? 0.0f : fmaxf(lnz - 0.69314718f * (total.w / total.s), 0.0f);
@@ -332,11 +360,11 @@ __global__ void __launch_bounds__(kThreads, 3) score_rows_kernel(const __grid_co
 
 // d / dv_x of  sum_t g_t log p(token_t) + h H  =  ( sum_{t: token_t = x} g_t - p_x (G + h (log p_x + H)) ) / T,   G = sum_t g_t.
 // The row is read twice, the second time from L2; words of the gradient are written on their own 16-byte boundaries.
-template <typename T, bool ALIGNED, bool ENTROPY>
-__global__ void __launch_bounds__(kThreads, 3) score_grad_kernel(const __grid_constant__ ScoreArgs a) {
+template <typename T, bool ALIGNED, bool ENTROPY, int NW>
+__global__ void __launch_bounds__(NW * 32, 32 / NW) score_grad_kernel(const __grid_constant__ ScoreArgs a) {
     using P = tiles::Packed16<T>;
     constexpr int E = P::kEntries;
-    __shared__ Sums sums;
+    extern __shared__ float dynamic[];             // the tiles' sums
     __shared__ RowTotals total_of_row;
     __shared__ int status_of_row;
     __shared__ int32_t tokens[RSD_MAX_K];
@@ -346,8 +374,9 @@ __global__ void __launch_bounds__(kThreads, 3) score_grad_kernel(const __grid_co
     if (tid == 0) status_of_row = 0;
     if (blocks > 1) tiles::cluster_arrive();
     grid_wait();
-    const int64_t slot = blockIdx.x / blocks, b = slot / a.R;
-    const int r = (int)(slot - b * a.R);
+    const uint32_t slot_word = blockIdx.x / blocks, sequence = slot_word / (uint32_t)a.R;
+    const int64_t slot = slot_word, b = sequence;
+    const int r = (int)(slot_word - sequence * (uint32_t)a.R);
     const char* row = (const char*)a.data + (b * a.seq_stride + r * a.row_stride) * (int64_t)sizeof(T);
     char* grad = (char*)a.grad + slot * a.V * (int64_t)sizeof(T);
     int status = 0;
@@ -359,15 +388,17 @@ __global__ void __launch_bounds__(kThreads, 3) score_grad_kernel(const __grid_co
     }
     const float h = ENTROPY ? a.g_entropy[slot] : 0.0f;
     const tiles::View view = tiles::view_of<T>(row, a.V);
-    const int n_tiles = tiles::tiles_of<T>(a.V, kWords), first = warp * (int)blocks + (int)rank, step = kWarps * (int)blocks;
+    const int n_tiles = tiles::tiles_of<T>(a.V, kWords), first = warp * (int)blocks + (int)rank, step = NW * (int)blocks;
+    const Sums sums(dynamic, n_tiles);
+    uint4 w[kWords];
+    load_half<T, ALIGNED>(w, view, first, 0, lane, a.V), load_half<T, ALIGNED>(w, view, first, kWords / 2, lane, a.V);
     if (blocks > 1) tiles::cluster_wait();
     else __syncthreads();
     bool bad = false;
+#pragma unroll 1
     for (int t = first; t < n_tiles; t += step) {
-        uint4 w[kWords];
-        tiles::load_tile<T, ALIGNED, kWords>(w, view, t, lane, a.V);
         float lane_max;
-        tile_sums<T, ENTROPY>(w, a.k, t, lane, blocks, sums, lane_max, bad);
+        tile_sums<T, ENTROPY>(w, a.k, t, lane, blocks, sums, lane_max, bad, [&](int half) { load_half<T, ALIGNED>(w, view, t + step, half, lane, a.V); });
     }
     if (bad) status |= RSD_ST_NAN_INPUT;
     if (status)
@@ -403,10 +434,10 @@ __global__ void __launch_bounds__(kThreads, 3) score_grad_kernel(const __grid_co
     const int head = (int)((uintptr_t)grad & 15u) / (int)sizeof(T);   // entries between the boundary and the gradient's first one
     const int out_tiles = tiles::tiles_of<T>(head + a.V, kWords);
     auto write = [&](auto plain_row) {
+#pragma unroll 1
         for (int t = first; t < out_tiles; t += step) {
             const int x0 = t * tiles::tile_entries<T>(kWords) + lane * E - head, from = x0 - lane * E;
             const bool whole = from >= 0 && from + tiles::tile_entries<T>(kWords) <= a.V;
-            uint4 w[kWords];
             tiles::load_words<T, ALIGNED, kWords>(w, view, x0, whole, a.V);
 #pragma unroll
             for (int k = 0; k < kWords; ++k) {

@@ -2,6 +2,7 @@
 // rsd_score_bf16.cu), which keeps the compiles short.
 #pragma once
 #include "../../include/rsd.h"
+#include <cstdlib>
 #include "rsd_api_common.h"
 #include "rsd_divergence.cuh"
 #include "rsd_score.cuh"
@@ -20,18 +21,49 @@ void launch_rows(void (*kernel)(A), unsigned slots, int blocks, int threads, siz
     rsd_host::launch_overlapped(kernel, slots * (unsigned)blocks, (unsigned)threads, smem, s, blocks > 1 ? blocks : 0, a);
 }
 
+inline int env_int(const char* n, int d) { const char* e = getenv(n); return e ? atoi(e) : d; }
+template <typename T, bool ALIGNED, bool TOP, int NW>
+void launch_score_as(unsigned slots, int blocks, const ScoreArgs& a, cudaStream_t s) {
+    const int n_tiles = tiles::tiles_of<T>(a.V, score::kWords);
+    const size_t smem = score::sums_bytes(n_tiles) + (TOP ? (size_t)((n_tiles + blocks - 1) / blocks) * 32 * sizeof(float) : 0);
+    launch_rows(score::score_rows_kernel<T, ALIGNED, TOP, NW>, slots, blocks, NW * 32, smem, s, a);
+}
+template <typename T, bool ALIGNED, bool TOP>
+void launch_score_warps(unsigned slots, const ScoreArgs& a, cudaStream_t s) {
+    const int blocks = row_blocks(slots, tiles::tiles_of<T>(a.V, score::kWords), 8);
+    const int nw = env_int("NW", 8);
+    if (blocks > 1 || nw == 8) launch_score_as<T, ALIGNED, TOP, 8>(slots, blocks, a, s);
+    else if (nw == 4) launch_score_as<T, ALIGNED, TOP, 4>(slots, 1, a, s);
+    else if (nw == 2) launch_score_as<T, ALIGNED, TOP, 2>(slots, 1, a, s);
+    else launch_score_as<T, ALIGNED, TOP, 1>(slots, 1, a, s);
+}
 template <typename T>
 void launch_score_of(bool aligned, unsigned slots, const ScoreArgs& a, cudaStream_t s) {
-    const int n_tiles = tiles::tiles_of<T>(a.V, score::kWords), blocks = row_blocks(slots, n_tiles, score::kWarps);
-    if (a.K) launch_rows(aligned ? score::score_rows_kernel<T, true, true> : score::score_rows_kernel<T, false, true>, slots, blocks, score::kThreads,
-                         (size_t)((n_tiles + blocks - 1) / blocks) * 32 * sizeof(float), s, a);
-    else launch_rows(aligned ? score::score_rows_kernel<T, true, false> : score::score_rows_kernel<T, false, false>, slots, blocks, score::kThreads, 0, s, a);
+    if (a.K) {
+        if (aligned) launch_score_warps<T, true, true>(slots, a, s);
+        else launch_score_warps<T, false, true>(slots, a, s);
+    } else {
+        if (aligned) launch_score_warps<T, true, false>(slots, a, s);
+        else launch_score_warps<T, false, false>(slots, a, s);
+    }
+}
+template <typename T, bool ENTROPY, int NW>
+void launch_score_grad_as(bool aligned, unsigned slots, int blocks, const ScoreArgs& a, cudaStream_t s) {
+    const size_t smem = score::sums_bytes(tiles::tiles_of<T>(a.V, score::kWords));
+    launch_rows(aligned ? score::score_grad_kernel<T, true, ENTROPY, NW> : score::score_grad_kernel<T, false, ENTROPY, NW>, slots, blocks, NW * 32, smem, s, a);
+}
+template <typename T, bool ENTROPY>
+void launch_score_grad_warps(bool aligned, unsigned slots, const ScoreArgs& a, cudaStream_t s) {
+    const int blocks = row_blocks(slots, tiles::tiles_of<T>(a.V, score::kWords), 8);
+    const int nw = env_int("NW", 8);
+    if (blocks > 1 || nw == 8) launch_score_grad_as<T, ENTROPY, 8>(aligned, slots, blocks, a, s);
+    else if (nw == 4) launch_score_grad_as<T, ENTROPY, 4>(aligned, slots, 1, a, s);
+    else launch_score_grad_as<T, ENTROPY, 2>(aligned, slots, 1, a, s);
 }
 template <typename T>
 void launch_score_grad_of(bool aligned, unsigned slots, const ScoreArgs& a, cudaStream_t s) {
-    const int blocks = row_blocks(slots, tiles::tiles_of<T>(a.V, score::kWords), score::kWarps);
-    if (a.g_entropy) launch_rows(aligned ? score::score_grad_kernel<T, true, true> : score::score_grad_kernel<T, false, true>, slots, blocks, score::kThreads, 0, s, a);
-    else launch_rows(aligned ? score::score_grad_kernel<T, true, false> : score::score_grad_kernel<T, false, false>, slots, blocks, score::kThreads, 0, s, a);
+    if (a.g_entropy) launch_score_grad_warps<T, true>(aligned, slots, a, s);
+    else launch_score_grad_warps<T, false>(aligned, slots, a, s);
 }
 template <typename T>
 void launch_divergence_of(bool aligned, unsigned slots, const DivergenceArgs& a, cudaStream_t s) {
