@@ -18,6 +18,7 @@ int check_batch(int B, int R) {
     if ((int64_t)B * R > 0x7FFFFFFF) return fail(RSD_ERR_UNSUPPORTED, "B * R too large");
     return RSD_OK;
 }
+float inverse(float temp) { return (float)std::min(1.0 / (double)temp, 3.0e38); }
 float exponent_scale(float temp) { return (float)std::min(1.4426950408889634 / (double)temp, 3.0e38); }   // log2(e) / T
 bool dense_aligned(const void* p, int V, int dtype) { return (uintptr_t)p % 16 == 0 && (int64_t)V * (dtype == RSD_F32 ? 4 : 2) % 16 == 0; }
 
@@ -26,7 +27,8 @@ rsd::ScoreArgs score_args(const rsd_rows* rows, int R, int V, int T, int K) {
     memset(&a, 0, sizeof(a));
     a.data = rows->data; a.seq_stride = rows->seq_stride; a.row_stride = rows->row_stride;
     a.R = R; a.V = V; a.T = T; a.K = K;
-    a.temp = temperature_of(rows); a.k = exponent_scale(a.temp);
+    const float temp = temperature_of(rows);
+    a.inv_temp = inverse(temp); a.k = exponent_scale(temp);
     return a;
 }
 rsd::DivergenceArgs divergence_args(const rsd_rows* draft, const rsd_rows* target, int R, int V) {
@@ -35,8 +37,8 @@ rsd::DivergenceArgs divergence_args(const rsd_rows* draft, const rsd_rows* targe
     a.draft = draft->data; a.draft_seq = draft->seq_stride; a.draft_row = draft->row_stride;
     a.target = target->data; a.target_seq = target->seq_stride; a.target_row = target->row_stride;
     a.R = R; a.V = V;
-    a.draft_temp = temperature_of(draft);
-    a.k_draft = exponent_scale(a.draft_temp); a.k_target = exponent_scale(temperature_of(target));
+    a.inv_draft_temp = inverse(temperature_of(draft));
+    a.k_draft = exponent_scale(temperature_of(draft)); a.k_target = exponent_scale(temperature_of(target));
     return a;
 }
 int check_pair(const rsd_rows* draft, const rsd_rows* target, int B, int R, int V) {

@@ -339,7 +339,7 @@ __global__ void __launch_bounds__(kThreads, 3) divergence_grad_kernel(const __gr
     const bool bad = read_rows<T, ALIGNED, REVERSE>(a, w, sm);
     const Result res = result_of(a, sm);
     const float g = a.g_kl ? a.g_kl[w.slot] : 0.0f, h = REVERSE ? a.g_reverse[w.slot] : 0.0f;
-    const float inv_temp = fminf(1.0f / a.draft_temp, 3.0e38f), gt = res.empty ? 0.0f : g * inv_temp, ht = res.empty || (REVERSE && res.reverse_infinite) ? 0.0f : h * inv_temp;
+    const float inv_temp = a.inv_draft_temp, gt = res.empty ? 0.0f : g * inv_temp, ht = res.empty || (REVERSE && res.reverse_infinite) ? 0.0f : h * inv_temp;
     const LogProb lp = log_prob(sm.total.mp, a.k_draft, res.log2_sp, res.empty), lq = log_prob(sm.total.mq, a.k_target, res.log2_sq, res.empty);
     const float scale_p = exp2f(lp.off), scale_q = exp2f(lq.off);
     // gt (p - q) + p ht (ln 2 (log2 p - log2 q) - KL(p||q)); rows that are equal give 0

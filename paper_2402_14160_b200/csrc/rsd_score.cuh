@@ -77,6 +77,11 @@ __device__ __forceinline__ void tile_sums(uint4 (&w)[kWords], float k, int t, in
     split_f32x2(s, s0, s1);
     split_f32x2(e, e0, e1);
     const float sum = tiles::warp_sum_two(s0 + s1, e0 + e1, lane);   // lanes 0 to 15 the first, the others the second
+    if (blocks == 1) {
+        if (lane == 0) sums.m[t] = m, sums.s[t] = sum;
+        if (ENTROPY && lane == 16) sums.w[t] = sum;
+        return;
+    }
     const uint32_t to = lane & 7;
     if (to < blocks) {
         if (lane < 8) tiles::store_at(&sums.s[t], to, sum);
@@ -98,17 +103,18 @@ __device__ __forceinline__ void load_half(uint4 (&w)[kWords], const tiles::View&
 }
 
 // The tiles' sums joined by one warp; every lane gets the result.
+template <bool ENTROPY>
 __device__ __forceinline__ RowTotals join(const Sums& sums, int n, float k, int lane) {
     float m = kNegInf;
     for (int t = lane; t < n; t += 32) m = fmaxf(m, sums.m[t]);
-    m = warp_max(m);
+    m = tiles::warp_max_nan(m);
     float s = 0.0f, w = 0.0f;
     for (int t = lane; t < n; t += 32) {
         const float mt = sums.m[t];
         if (mt == kNegInf) continue;
         const float d = fmaxf((mt - m) * k, tiles::kFarBelow) - tiles::rounded_off(mt, k), f = ex2_approx(d);
         s = fmaf(f, sums.s[t], s);
-        w = fmaf(f, fmaf(d, sums.s[t], sums.w[t]), w);
+        if (ENTROPY) w = fmaf(f, fmaf(d, sums.s[t], sums.w[t]), w);
     }
     const float sum = tiles::warp_sum_two(s, w, lane);
     return {m, __shfl_sync(0xFFFFFFFFu, sum, 0), __shfl_sync(0xFFFFFFFFu, sum, 16)};
@@ -310,7 +316,7 @@ __global__ void __launch_bounds__(NW * 32, 32 / NW) score_rows_kernel(const __gr
     if constexpr (TOP) block_bound<NW>(top_store, even, odd, a.K, rank, blocks);
     tiles::row_barrier(blocks);
     if (rank == 0 && warp == 0) {
-        const RowTotals t = join(sums, n_tiles, a.k, lane);
+        const RowTotals t = join<true>(sums, n_tiles, a.k, lane);
         if (lane == 0) total_of_row = t;
     }
     if constexpr (TOP) {
@@ -329,7 +335,7 @@ __global__ void __launch_bounds__(NW * 32, 32 / NW) score_rows_kernel(const __gr
     const RowTotals total = total_of_row;
     const bool none = !there || total.m == kNegInf;
     const float lnz = none ? 0.0f : logf(total.s);
-    auto logprob = [&](float v) { return v == kNegInf ? kNegInf : (v - total.m) / a.temp - lnz; };
+    auto logprob = [&](float v) { return v == kNegInf ? kNegInf : fmaf(v - total.m, a.inv_temp, -lnz); };
     if (tid < a.T) {
         if (a.out_logprob) a.out_logprob[slot * a.T + tid] = there && token >= 0 ? logprob(value) : 0.0f;
         if (a.out_token) a.out_token[slot] = there ? token : -1;
@@ -352,20 +358,39 @@ __global__ void __launch_bounds__(NW * 32, 32 / NW) score_rows_kernel(const __gr
         for (int i = n + tid; i < a.K; i += NW * 32) a.out_top_token[slot * a.K + i] = -1, a.out_top_logprob[slot * a.K + i] = kNegInf;
     }
     if (tid == 0) {
-        if (a.out_entropy) a.out_entropy[slot] = none ? 0.0f : fmaxf(lnz - 0.69314718f * (total.w / total.s), 0.0f);
+        if (a.out_entropy) a.out_entropy[slot] = none ? 0.0f : fmaxf(lnz - 0.69314718f * __fdividef(total.w, total.s), 0.0f);
         a.status[slot] = status_of_row | (there && none ? RSD_ST_EMPTY_ROW : 0) | (few ? RSD_ST_FEWER_THAN_K : 0);
     }
     grid_started();
 }
 
 // d / dv_x of  sum_t g_t log p(token_t) + h H  =  ( sum_{t: token_t = x} g_t - p_x (G + h (log p_x + H)) ) / T,   G = sum_t g_t.
-// The row is read twice, the second time from L2; words of the gradient are written on their own 16-byte boundaries.
+// A block has consecutive tiles of its row and keeps them in shared memory for the second sweep (read again from L2, the
+// gradient's own words pushed two thirds of the rows out to memory); words of the gradient are written on their own 16-byte boundaries.
+struct Slope {                     // gradient of an entry without a token: p (c0 + c1 log2 p),   log2 p = v k - c (plain rows) or (v - m) k - c
+    float m, c, c0, c1, inv_temp;
+    int plain, none;
+};
+__device__ __forceinline__ Slope slope_of(const RowTotals& total, float G, float h, float inv_temp, float k) {
+    Slope f;
+    f.m = total.m, f.inv_temp = inv_temp;
+    f.none = total.m == kNegInf, f.plain = tiles::plain_tile(total.m, k);
+    const float log2s = f.none ? 0.0f : log2f(total.s), H = f.none ? 0.0f : 0.69314718f * (log2s - __fdividef(total.w, total.s));
+    // what c loses when it is rounded goes into the factors
+    f.c = f.plain ? fmaf(total.m, k, log2s) : log2s;
+    const float off = f.plain ? -(fmaf(total.m, k, -f.c) + log2s) : 0.0f, scale = ex2_approx(off);
+    f.c1 = f.none ? 0.0f : -h * 0.69314718f * inv_temp;
+    f.c0 = f.none ? 0.0f : fmaf(f.c1, off, -(G + h * H) * inv_temp) * scale;
+    f.c1 *= scale;
+    return f;
+}
+
 template <typename T, bool ALIGNED, bool ENTROPY, int NW>
 __global__ void __launch_bounds__(NW * 32, 32 / NW) score_grad_kernel(const __grid_constant__ ScoreArgs a) {
     using P = tiles::Packed16<T>;
-    constexpr int E = P::kEntries;
-    extern __shared__ float dynamic[];             // the tiles' sums
-    __shared__ RowTotals total_of_row;
+    constexpr int E = P::kEntries, kTile = tiles::tile_entries<T>(kWords), kHeld = tiles::kHeldTile<kWords>;
+    extern __shared__ __align__(16) unsigned char dynamic_bytes[];   // the block's tiles, then all tiles' sums
+    __shared__ Slope slope_of_row;
     __shared__ int status_of_row;
     __shared__ int32_t tokens[RSD_MAX_K];
     __shared__ float weights[RSD_MAX_K];
@@ -373,109 +398,113 @@ __global__ void __launch_bounds__(NW * 32, 32 / NW) score_grad_kernel(const __gr
     const uint32_t rank = tiles::cluster_rank(), blocks = tiles::cluster_blocks();
     if (tid == 0) status_of_row = 0;
     if (blocks > 1) tiles::cluster_arrive();
-    grid_wait();
-    const uint32_t slot_word = blockIdx.x / blocks, sequence = slot_word / (uint32_t)a.R;
-    const int64_t slot = slot_word, b = sequence;
-    const int r = (int)(slot_word - sequence * (uint32_t)a.R);
-    const char* row = (const char*)a.data + (b * a.seq_stride + r * a.row_stride) * (int64_t)sizeof(T);
-    char* grad = (char*)a.grad + slot * a.V * (int64_t)sizeof(T);
-    int status = 0;
-    if (tid < a.T) {
-        int32_t token = a.token[slot * a.T + tid];
-        if (token >= a.V) token = -1, status |= RSD_ST_BAD_INDEX;
-        tokens[tid] = token;
-        weights[tid] = token >= 0 ? a.g_logprob[slot * a.T + tid] : 0.0f;
-    }
-    const float h = ENTROPY ? a.g_entropy[slot] : 0.0f;
-    const tiles::View view = tiles::view_of<T>(row, a.V);
-    const int n_tiles = tiles::tiles_of<T>(a.V, kWords), first = warp * (int)blocks + (int)rank, step = NW * (int)blocks;
-    const Sums sums(dynamic, n_tiles);
-    uint4 w[kWords];
-    load_half<T, ALIGNED>(w, view, first, 0, lane, a.V), load_half<T, ALIGNED>(w, view, first, kWords / 2, lane, a.V);
-    if (blocks > 1) tiles::cluster_wait();
     else __syncthreads();
+    grid_wait();
+    const uint32_t slot = blockIdx.x / blocks, sequence = slot / (uint32_t)a.R;
+    const char* row = (const char*)a.data + (sequence * a.seq_stride + (slot - sequence * (uint32_t)a.R) * a.row_stride) * (int64_t)sizeof(T);
+    const tiles::View view = tiles::view_of<T>(row, a.V);
+    const int n_tiles = tiles::tiles_of<T>(a.V, kWords), each = (n_tiles + (int)blocks - 1) / (int)blocks;   // tiles of a block
+    const int t0 = min((int)rank * each, n_tiles), t1 = min(t0 + each, n_tiles);
+    const uint32_t held = smem_u32(dynamic_bytes);
+    const Sums sums((float*)(dynamic_bytes + each * kHeld), n_tiles);
+    for (int t = t0 + warp; t < t1; t += NW) {
+        tiles::fetch_tile<ALIGNED, kWords>(held + (t - t0) * kHeld, view, t, lane);
+        tiles::copies_sent();
+    }
+    char* grad = (char*)a.grad + (int64_t)slot * a.V * (int64_t)sizeof(T);
+    int status = 0;
+    int32_t token = -1;                            // (used behind the first sweep)
+    float weight = 0.0f, h = 0.0f;
+    if (tid < a.T) token = a.token[(int64_t)slot * a.T + tid], weight = a.g_logprob[(int64_t)slot * a.T + tid];
+    if (ENTROPY) h = a.g_entropy[slot];
+    if (blocks > 1) tiles::cluster_wait();
     bool bad = false;
 #pragma unroll 1
-    for (int t = first; t < n_tiles; t += step) {
+    for (int t = t0 + warp; t < t1; t += NW) {
+        uint4 w[kWords];
+        tiles::copies_landed((t1 - 1 - t) / NW);
+        __syncwarp();
+        tiles::read_tile<T, ALIGNED, kWords>(w, held + (t - t0) * kHeld, view, t, lane, a.V);
         float lane_max;
-        tile_sums<T, ENTROPY>(w, a.k, t, lane, blocks, sums, lane_max, bad, [&](int half) { load_half<T, ALIGNED>(w, view, t + step, half, lane, a.V); });
+        tile_sums<T, ENTROPY>(w, a.k, t, lane, blocks, sums, lane_max, bad, [](int) {});
     }
     if (bad) status |= RSD_ST_NAN_INPUT;
+    if (token >= a.V) token = -1, status |= RSD_ST_BAD_INDEX;
+    if (token < 0) weight = 0.0f;
+    if (tid < a.T) tokens[tid] = token, weights[tid] = weight;
     if (status)
         for (uint32_t i = 0; i < blocks; ++i) tiles::or_at(&status_of_row, i, status);
     tiles::row_barrier(blocks);
     if (warp == 0) {
-        const RowTotals t = join(sums, n_tiles, a.k, lane);
-        if (lane == 0) total_of_row = t;
+        const RowTotals total = join<ENTROPY>(sums, n_tiles, a.k, lane);
+        float G = 0.0f;
+        for (int t = 0; t < a.T; ++t) G += weights[t];
+        const Slope f = slope_of(total, G, h, a.inv_temp, a.k);
+        if (lane == 0) slope_of_row = f;
     }
     __syncthreads();
-    const RowTotals total = total_of_row;
+    const Slope f = slope_of_row;
     bad = status_of_row & RSD_ST_NAN_INPUT;
-    const bool none = total.m == kNegInf, plain = tiles::plain_tile(total.m, a.k);
-    float G = 0.0f;
-    for (int t = 0; t < a.T; ++t) G += weights[t];
-    const float inv_temp = fminf(1.0f / a.temp, 3.0e38f), log2s = none ? 0.0f : log2f(total.s);
-    const float H = ENTROPY && !none ? 0.69314718f * (log2s - total.w / total.s) : 0.0f;
-    // log2 p = v k - c + off, where off is what c = m k + log2 S loses when it is rounded; p and the factor that it is multiplied by take it in
-    const double exact = plain ? (double)total.m * (double)a.k + (double)log2s : (double)log2s;
-    const float c = (float)exact, off = (float)((double)c - exact), scale = exp2f(off);
-    // gradient of an entry without a token: p (c0 + c1 log2 p)
-    float c1 = none ? 0.0f : -h * 0.69314718f * inv_temp, c0 = none ? 0.0f : fmaf(c1, off, -(G + h * H) * inv_temp);
-    c1 *= scale, c0 *= scale;
-    const unsigned long long minus_m = tiles::both(none || plain ? 0.0f : -total.m), kk = tiles::both(a.k), minus_c = tiles::both(-c), cc0 = tiles::both(c0), cc1 = tiles::both(c1);
+    const unsigned long long minus_m = tiles::both(f.none || f.plain ? 0.0f : -f.m), kk = tiles::both(a.k), minus_c = tiles::both(-f.c), c0 = tiles::both(f.c0), c1 = tiles::both(f.c1);
     auto slope = [&](unsigned long long v, auto plain_row) {
         float x, y;
         const unsigned long long l = fma_f32x2(decltype(plain_row)::value ? v : add_f32x2(v, minus_m), kk, minus_c);
         split_f32x2(l, x, y);
         if (ENTROPY && !decltype(plain_row)::value) x = fmaxf(x, tiles::kFarBelow), y = fmaxf(y, tiles::kFarBelow);
         const unsigned long long p = f32x2(ex2_approx(x), ex2_approx(y));
-        return tiles::mul_f32x2(p, ENTROPY ? fma_f32x2(f32x2(x, y), cc1, cc0) : cc0);
+        return tiles::mul_f32x2(p, ENTROPY ? fma_f32x2(f32x2(x, y), c1, c0) : c0);
     };
-    const int head = (int)((uintptr_t)grad & 15u) / (int)sizeof(T);   // entries between the boundary and the gradient's first one
-    const int out_tiles = tiles::tiles_of<T>(head + a.V, kWords);
+    const int head = ALIGNED ? 0 : (int)((uintptr_t)grad & 15u) / (int)sizeof(T);   // entries between the boundary and the gradient's first one
+    auto word = [&](int x, bool whole, auto plain_row) {
+        uint4 v = tiles::held_word<T, ALIGNED, kWords>(held, view, t0, t1, x, a.V);
+        if (bad) {
+            bool ignored = false;
+            P::clean(v, ignored);
+        }
+        if (ENTROPY && decltype(plain_row)::value) v = P::raised(v);
+        const uint4 g = P::make([&](int i) { return slope(P::pair(v, i), plain_row); });
+        if (whole || (x >= 0 && x + E <= a.V)) {
+            __stcs((uint4*)(grad + (int64_t)x * (int)sizeof(T)), g);
+        } else {
+            for (int i = 0; i < E; ++i)
+                if (x + i >= 0 && x + i < a.V) P::store(grad, x + i, P::get(g, i));
+        }
+    };
     auto write = [&](auto plain_row) {
+        const int last = t1 == n_tiles ? tiles::tiles_of<T>(head + a.V, kWords) : t1;   // tiles of the gradient: `head` entries ahead of the row's
 #pragma unroll 1
-        for (int t = first; t < out_tiles; t += step) {
-            const int x0 = t * tiles::tile_entries<T>(kWords) + lane * E - head, from = x0 - lane * E;
-            const bool whole = from >= 0 && from + tiles::tile_entries<T>(kWords) <= a.V;
-            tiles::load_words<T, ALIGNED, kWords>(w, view, x0, whole, a.V);
-#pragma unroll
-            for (int k = 0; k < kWords; ++k) {
-                if (bad) {
-                    bool ignored = false;
-                    P::clean(w[k], ignored);
-                }
-                if (ENTROPY && decltype(plain_row)::value) w[k] = P::raised(w[k]);
-                const uint4 g = P::make([&](int i) { return slope(P::pair(w[k], i), plain_row); });
-                const int x = x0 + k * 32 * E;
-                if (whole || (x >= 0 && x + E <= a.V)) {
-                    *(uint4*)(grad + (int64_t)x * (int)sizeof(T)) = g;
-                } else {
-                    for (int i = 0; i < E; ++i)
-                        if (x + i >= 0 && x + i < a.V) P::store(grad, x + i, P::get(g, i));
-                }
+        for (int t = t0 + warp; t < last && t0 < t1; t += NW) {
+            const int x = t * kTile - head + lane * E;
+            if (t * kTile >= head && (t + 1) * kTile - head <= a.V) {
+#pragma unroll 4
+                for (int k = 0; k < kWords; ++k) word(x + k * 32 * E, true, plain_row);
+            } else {
+#pragma unroll 1
+                for (int k = 0; k < kWords; ++k)
+                    if (x + k * 32 * E < a.V) word(x + k * 32 * E, false, plain_row);
             }
         }
     };
-    if (plain) write(std::true_type());
+    if (f.plain) write(std::true_type());
     else write(std::false_type());
     __syncthreads();
     // The tokens' entries again, with their own weights, by the block that wrote them; a token given twice has both.
-    if (tid < a.T && tokens[tid] >= 0 && (uint32_t)((tokens[tid] + head) / tiles::tile_entries<T>(kWords)) % blocks == rank) {
-        const int32_t x = tokens[tid];
+    if (token >= 0 && min((token + head) / kTile, n_tiles - 1) / each == (int)rank) {
+        const int32_t x = token;
         float own = 0.0f;
         bool first_of_it = true;
         for (int t = 0; t < a.T; ++t)
             if (tokens[t] == x) own += weights[t], first_of_it = first_of_it && t >= tid;
         if (first_of_it) {
-            const float v = entry<T>(row, x);
+            const int in_tiles = view.first + x * (int)sizeof(T) - t0 * kWords * 512, tile = min(in_tiles / (kWords * 512), t1 - t0 - 1);
+            const float v = in_tiles >= 0 ? entry<T>(dynamic_bytes + in_tiles + tile * 16, 0) : entry<T>(row, x);
             float rest, ignored;
-            if (plain) split_f32x2(slope(tiles::both(fmaxf(v, tiles::kLow)), std::true_type()), rest, ignored);
+            if (f.plain) split_f32x2(slope(tiles::both(fmaxf(v, tiles::kLow)), std::true_type()), rest, ignored);
             else split_f32x2(slope(tiles::both(v), std::false_type()), rest, ignored);
-            P::store(grad, x, none ? 0.0f : fmaf(own, inv_temp, rest));
+            P::store(grad, x, f.none ? 0.0f : fmaf(own, f.inv_temp, rest));
         }
     }
-    if (rank == 0 && tid == 0) a.status[slot] = status_of_row | (none ? RSD_ST_EMPTY_ROW : 0);
+    if (rank == 0 && tid == 0) a.status[slot] = status_of_row | (f.none ? RSD_ST_EMPTY_ROW : 0);
     grid_started();
 }
 

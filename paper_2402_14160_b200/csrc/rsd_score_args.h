@@ -13,7 +13,7 @@ struct ScoreArgs {
     const int32_t* token;          // [B][R][T] or null
     // the path that a verification accepted, in place of row_index and token (R = L + 1, T = 1)
     const int32_t *accepted_len, *accepted_node, *accepted_token, *last_token;
-    float temp, k;                 // temperature, log2(e) / temperature
+    float inv_temp, k;             // 1 / temperature, log2(e) / temperature; finite
     float *out_logprob, *out_entropy, *out_top_logprob;
     int32_t *out_token, *out_top_token, *status;
     // gradient
@@ -26,7 +26,7 @@ struct DivergenceArgs {
     int64_t draft_seq, draft_row, target_seq, target_row;    // strides in entries
     int R, V;
     float k_draft, k_target;                                 // log2(e) / temperature
-    float draft_temp;
+    float inv_draft_temp;
     float *out_kl, *out_reverse, *out_overlap;
     int32_t* status;
     const float *g_kl, *g_reverse;

@@ -47,23 +47,37 @@ void launch_score_of(bool aligned, unsigned slots, const ScoreArgs& a, cudaStrea
         else launch_score_warps<T, false, false>(slots, a, s);
     }
 }
-template <typename T, bool ENTROPY, int NW>
-void launch_score_grad_as(bool aligned, unsigned slots, int blocks, const ScoreArgs& a, cudaStream_t s) {
-    const size_t smem = score::sums_bytes(tiles::tiles_of<T>(a.V, score::kWords));
-    launch_rows(aligned ? score::score_grad_kernel<T, true, ENTROPY, NW> : score::score_grad_kernel<T, false, ENTROPY, NW>, slots, blocks, NW * 32, smem, s, a);
+// Blocks of a row whose tiles they keep in shared memory: as few as leave three blocks on an SM, and more where few rows leave SMs idle.
+constexpr int kHeldBytes = 68 * 1024, kMostHeldBytes = 200 * 1024;
+inline int holding_blocks(unsigned slots, int n_tiles, int tile_bytes, int warps) {
+    int blocks = row_blocks(slots, n_tiles, warps);
+    while (blocks < tiles::kMaxBlocks && (n_tiles + blocks - 1) / blocks * tile_bytes > kHeldBytes) blocks *= 2;
+    return blocks;
 }
-template <typename T, bool ENTROPY>
-void launch_score_grad_warps(bool aligned, unsigned slots, const ScoreArgs& a, cudaStream_t s) {
-    const int blocks = row_blocks(slots, tiles::tiles_of<T>(a.V, score::kWords), 8);
+template <typename T, bool ALIGNED, bool ENTROPY, int NW>
+void launch_score_grad_as(unsigned slots, int blocks, const ScoreArgs& a, cudaStream_t s) {
+    constexpr int kTileBytes = tiles::kHeldTile<score::kWords>;
+    const int n_tiles = tiles::tiles_of<T>(a.V, score::kWords);
+    if (!rsd_host::raise_shared_memory<score::score_grad_kernel<T, ALIGNED, ENTROPY, NW>>(kMostHeldBytes)) return;
+    launch_rows(score::score_grad_kernel<T, ALIGNED, ENTROPY, NW>, slots, blocks, NW * 32, (size_t)((n_tiles + blocks - 1) / blocks) * kTileBytes + score::sums_bytes(n_tiles), s, a);
+}
+template <typename T, bool ALIGNED, bool ENTROPY>
+void launch_score_grad_warps(unsigned slots, const ScoreArgs& a, cudaStream_t s) {
+    const int n_tiles = tiles::tiles_of<T>(a.V, score::kWords), blocks = holding_blocks(slots, n_tiles, tiles::kHeldTile<score::kWords>, 8);
     const int nw = env_int("NW", 8);
-    if (blocks > 1 || nw == 8) launch_score_grad_as<T, ENTROPY, 8>(aligned, slots, blocks, a, s);
-    else if (nw == 4) launch_score_grad_as<T, ENTROPY, 4>(aligned, slots, 1, a, s);
-    else launch_score_grad_as<T, ENTROPY, 2>(aligned, slots, 1, a, s);
+    if (blocks > 1 || nw == 8) launch_score_grad_as<T, ALIGNED, ENTROPY, 8>(slots, blocks, a, s);
+    else if (nw == 4) launch_score_grad_as<T, ALIGNED, ENTROPY, 4>(slots, 1, a, s);
+    else launch_score_grad_as<T, ALIGNED, ENTROPY, 2>(slots, 1, a, s);
 }
 template <typename T>
 void launch_score_grad_of(bool aligned, unsigned slots, const ScoreArgs& a, cudaStream_t s) {
-    if (a.g_entropy) launch_score_grad_warps<T, true>(aligned, slots, a, s);
-    else launch_score_grad_warps<T, false>(aligned, slots, a, s);
+    if (a.g_entropy) {
+        if (aligned) launch_score_grad_warps<T, true, true>(slots, a, s);
+        else launch_score_grad_warps<T, false, true>(slots, a, s);
+    } else {
+        if (aligned) launch_score_grad_warps<T, true, false>(slots, a, s);
+        else launch_score_grad_warps<T, false, false>(slots, a, s);
+    }
 }
 template <typename T>
 void launch_divergence_of(bool aligned, unsigned slots, const DivergenceArgs& a, cudaStream_t s) {

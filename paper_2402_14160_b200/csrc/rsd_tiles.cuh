@@ -252,6 +252,79 @@ __device__ __forceinline__ void load_tile(uint4 (&w)[KW], const View& v, int t, 
     load_words<T, ALIGNED, KW>(w, v, t * tile_entries<T>(KW) + lane * Packed16<T>::kEntries, (t + 1) * tile_entries<T>(KW) <= V, V);
 }
 
+// ---- tiles held in shared memory ---------------------------------------------------------------------------------------------------
+// A held tile is KW * 32 granules of the row and, so that a row off the boundaries can be shifted, the first granule of the next tile.  The copies go on without
+// registers: a block asks for all its tiles at once and a warp waits for its own.
+template <int KW>
+constexpr int kHeldTile = KW * 512 + 16;
+__device__ __forceinline__ void copy_granule(uint32_t to, const char* from) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copies_sent() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void copies_landed(int later) {   // all but (at most) the last `later` groups of this thread
+    if (later >= 3) asm volatile("cp.async.wait_group 3;" ::: "memory");
+    else if (later == 2) asm volatile("cp.async.wait_group 2;" ::: "memory");
+    else if (later == 1) asm volatile("cp.async.wait_group 1;" ::: "memory");
+    else asm volatile("cp.async.wait_group 0;" ::: "memory");
+}
+template <bool ALIGNED, int KW>
+__device__ __forceinline__ void fetch_tile(uint32_t to, const View& v, int t, int lane) {
+    const int g = t * KW * 32 + lane;
+    const char* from = v.base + (int64_t)g * 16;
+    if ((t + 1) * KW * 32 <= v.last) {
+#pragma unroll
+        for (int k = 0; k < KW; ++k) copy_granule(to + (k * 32 + lane) * 16, from + k * 512);
+        if (!ALIGNED && lane == 0) copy_granule(to + KW * 512, from + KW * 512);
+    } else {
+#pragma unroll
+        for (int k = 0; k < KW; ++k)
+            if (g + k * 32 <= v.last) copy_granule(to + (k * 32 + lane) * 16, from + k * 512);
+    }
+}
+__device__ __forceinline__ uint4 held_granule(uint32_t at) {
+    uint4 w;
+    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w) : "r"(at) : "memory");
+    return w;
+}
+// The words of a held tile, entries outside the row as -inf.  (The warp's copies have landed for all its lanes.)
+template <typename T, bool ALIGNED, int KW>
+__device__ __forceinline__ void read_tile(uint4 (&w)[KW], uint32_t at, const View& v, int t, int lane, int V) {
+    constexpr int E = Packed16<T>::kEntries;
+    at += lane * 16;
+#pragma unroll
+    for (int k = 0; k < KW; ++k) w[k] = held_granule(at + k * 512);
+    if (!ALIGNED && v.first) {
+        with_shift(v.first, [&](auto q) {
+#pragma unroll
+            for (int k = 0; k < KW; ++k) w[k] = shifted<decltype(q)::value>(w[k], held_granule(at + k * 512 + 16), (v.first & 3) * 8);
+        });
+    }
+    if ((t + 1) * tile_entries<T>(KW) > V) {
+#pragma unroll
+        for (int k = 0; k < KW; ++k) {
+            const int x0 = ((t * KW + k) * 32 + lane) * E;
+            if (x0 >= V) w[k] = Packed16<T>::masked();
+            else if (x0 + E > V) Packed16<T>::keep(w[k], 0, V - x0);
+        }
+    }
+}
+// Tiles t0 .. t1 - 1 of a row as a block holds them, read by words of another boundary: entries x0 .. x0 + E - 1, where x0 lies `shift` bytes behind a granule.
+// Entries outside the row are undefined.
+template <typename T, bool ALIGNED, int KW>
+__device__ __forceinline__ uint4 held_word(uint32_t held, const View& v, int t0, int t1, int x0, int V) {
+    const int at = v.first + x0 * (int)sizeof(T), shift = at & 15, g = at >> 4, local = g - t0 * KW * 32;
+    if (ALIGNED) return held_granule(held + local * 16 + (local / (KW * 32)) * 16);
+    if (local < 0 || g + (shift != 0) > t1 * KW * 32) return load_word<T, false>(v, x0, V);   // another block's
+    const int tile = min(local / (KW * 32), t1 - t0 - 1);
+    const uint32_t a = held + local * 16 + tile * 16;
+    uint4 w = held_granule(a);
+    if (shift) {
+        const uint4 b = held_granule(a + 16);            // (the granule behind a tile's last one is held with it)
+        with_shift(shift, [&](auto q) { w = shifted<decltype(q)::value>(w, b, (shift & 3) * 8); });
+    }
+    return w;
+}
+
 // ---- a row's blocks: one, or a cluster of up to eight that deal out its tiles -----------------------------------------------------------------
 constexpr int kMaxBlocks = 8;
 __device__ __forceinline__ uint32_t cluster_rank() {
