@@ -19,6 +19,7 @@ struct ScoreArgs {
     // gradient
     const float *g_logprob, *g_entropy;
     void* grad;
+    int slots;                     // B R
 };
 
 struct DivergenceArgs {
@@ -31,6 +32,7 @@ struct DivergenceArgs {
     int32_t* status;
     const float *g_kl, *g_reverse;
     void* grad;
+    int slots;
 };
 
 // `slots` rows (or pairs of rows), a block or a cluster of blocks each.  aligned: rows (and gradient rows) start on 16-byte boundaries.
