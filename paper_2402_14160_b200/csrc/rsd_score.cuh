@@ -385,162 +385,134 @@ __device__ __forceinline__ Slope slope_of(const RowTotals& total, float G, float
     return f;
 }
 
-// The row of a slot, and the tiles of it that a block has.
-struct GradRow {
-    tiles::View view;
-    int64_t slot;
-};
-template <typename T>
-__device__ __forceinline__ GradRow grad_row(const ScoreArgs& a, uint32_t slot) {
-    const uint32_t sequence = slot / (uint32_t)a.R;
-    const char* row = (const char*)a.data + (sequence * a.seq_stride + (slot - sequence * (uint32_t)a.R) * a.row_stride) * (int64_t)sizeof(T);
-    return {tiles::view_of<T>(row, a.V), slot};
-}
-
-// Blocks stay for one row after the other: where a warp is through with a tile, it asks for the same tile of the block's next row.
 template <typename T, bool ALIGNED, bool ENTROPY, int NW>
 __global__ void __launch_bounds__(NW * 32, 24 / NW) score_grad_kernel(const __grid_constant__ ScoreArgs a) {
     using P = tiles::Packed16<T>;
     constexpr int E = P::kEntries, kTile = tiles::tile_entries<T>(kWords), kHeld = tiles::kHeldTile<kWords>;
-    extern __shared__ __align__(16) unsigned char dynamic_bytes[];   // the block's tiles, then all tiles' sums of this row and the next one
+    extern __shared__ __align__(16) unsigned char dynamic_bytes[];   // the block's tiles, then all tiles' sums
     __shared__ Slope slope_of_row;
-    __shared__ int status_words[3];                // of this row, the next one and the one after
-    __shared__ int32_t tokens_of[2][RSD_MAX_K];    // of this row and the next one; absent: -1
-    __shared__ float weights_of[2][RSD_MAX_K];
+    __shared__ int status_of_row;
+    __shared__ int32_t tokens[RSD_MAX_K];          // absent: -1
+    __shared__ float weights[RSD_MAX_K];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const uint32_t rank = tiles::cluster_rank(), blocks = tiles::cluster_blocks(), rows = gridDim.x / blocks;   // rows under way
-    if (tid < 3) status_words[tid] = 0;
+    const uint32_t rank = tiles::cluster_rank(), blocks = tiles::cluster_blocks();
+    if (tid == 0) status_of_row = 0;
     if (blocks > 1) tiles::cluster_arrive();
     else __syncthreads();
     grid_wait();
+    const uint32_t slot = blockIdx.x / blocks, sequence = slot / (uint32_t)a.R;
+    const char* row = (const char*)a.data + (sequence * a.seq_stride + (slot - sequence * (uint32_t)a.R) * a.row_stride) * (int64_t)sizeof(T);
+    const tiles::View view = tiles::view_of<T>(row, a.V);
     const int n_tiles = tiles::tiles_of<T>(a.V, kWords), each = (n_tiles + (int)blocks - 1) / (int)blocks;   // tiles of a block
     const int t0 = min((int)rank * each, n_tiles), t1 = min(t0 + each, n_tiles);
     const uint32_t held = smem_u32(dynamic_bytes);
-    float* const all_sums = (float*)(dynamic_bytes + each * kHeld);
-    uint32_t slot = blockIdx.x / blocks;
-    GradRow row = grad_row<T>(a, slot);
-    auto fetch = [&](const GradRow& of, int t) {
-        tiles::fetch_tile<ALIGNED, kWords>(held + (t - t0) * kHeld, of.view, t, lane);
+    const Sums sums((float*)(dynamic_bytes + each * kHeld), n_tiles);
+    for (int t = t0 + warp; t < t1; t += NW) {
+        tiles::fetch_tile<ALIGNED, kWords>(held + (t - t0) * kHeld, view, t, lane);
         tiles::copies_sent();
-    };
-    for (int t = t0 + warp; t < t1; t += NW) fetch(row, t);
+    }
+    int32_t token = -1;                            // lane t of the first warp has token t
+    float weight = 0.0f, h = 0.0f;
+    if (tid < a.T) token = a.token[(int64_t)slot * a.T + tid], weight = a.g_logprob[(int64_t)slot * a.T + tid];
+    if (ENTROPY && warp == 0) h = a.g_entropy[slot];
     if (blocks > 1) tiles::cluster_wait();
+    bool bad = false;
 #pragma unroll 1
-    for (uint32_t n = 0;; ++n) {
-        const tiles::View view = row.view;
-        const bool more = slot + rows < (uint32_t)a.slots;
-        const Sums sums(all_sums + (n & 1) * 3 * n_tiles, n_tiles);
-        int* const status_of_row = &status_words[n % 3];
-        char* const grad = (char*)a.grad + row.slot * a.V * (int64_t)sizeof(T);
-        int32_t* const tokens = tokens_of[n & 1];
-        float* const weights = weights_of[n & 1];
-        int32_t token = -1;                        // lane t of the first warp has token t
-        float weight = 0.0f, h = 0.0f;
-        if (tid < a.T) token = a.token[row.slot * a.T + tid], weight = a.g_logprob[row.slot * a.T + tid];
-        if (ENTROPY && warp == 0) h = a.g_entropy[row.slot];
-        bool bad = false;
-#pragma unroll 1
-        for (int t = t0 + warp; t < t1; t += NW) {
-            uint4 w[kWords];
-            tiles::copies_landed((t1 - 1 - t) / NW);
-            __syncwarp();
-            tiles::read_tile<T, ALIGNED, kWords>(w, held + (t - t0) * kHeld, view, t, lane, a.V);
-            float lane_max;
-            tile_sums<T, ENTROPY>(w, a.k, t, lane, blocks, sums, lane_max, bad, [](int) {});
-        }
-        int status = bad ? RSD_ST_NAN_INPUT : 0;
-        if (token >= a.V) token = -1, status |= RSD_ST_BAD_INDEX;
-        if (token < 0) weight = 0.0f;
-        if (tid < a.T) tokens[tid] = token, weights[tid] = weight;
-        if (status)
-            for (uint32_t i = 0; i < blocks; ++i) tiles::or_at(status_of_row, i, status);
-        float G = weight;
-        if (warp == 0) {
+    for (int t = t0 + warp; t < t1; t += NW) {
+        uint4 w[kWords];
+        tiles::copies_landed((t1 - 1 - t) / NW);
+        __syncwarp();
+        tiles::read_tile<T, ALIGNED, kWords>(w, held + (t - t0) * kHeld, view, t, lane, a.V);
+        float lane_max;
+        tile_sums<T, ENTROPY>(w, a.k, t, lane, blocks, sums, lane_max, bad, [](int) {});
+    }
+    int status = bad ? RSD_ST_NAN_INPUT : 0;
+    if (token >= a.V) token = -1, status |= RSD_ST_BAD_INDEX;
+    if (token < 0) weight = 0.0f;
+    if (tid < a.T) tokens[tid] = token, weights[tid] = weight;
+    if (status)
+        for (uint32_t i = 0; i < blocks; ++i) tiles::or_at(&status_of_row, i, status);
+    float G = weight;
+    if (warp == 0) {
 #pragma unroll
-            for (int o = 16; o > 0; o >>= 1) G += __shfl_xor_sync(0xFFFFFFFFu, G, o);
-        }
-        tiles::row_barrier(blocks);
-        if (warp == 0) {
-            const Slope f = slope_of(join<ENTROPY>(sums, n_tiles, a.k, lane), G, h, a.inv_temp, a.k);
-            if (lane == 0) {
-                slope_of_row = f;
-                status_words[(n + 2) % 3] = 0;
-                if (rank == 0) a.status[slot] = *status_of_row | (f.none ? RSD_ST_EMPTY_ROW : 0);
-            }
-        }
-        __syncthreads();
-        const Slope f = slope_of_row;
-        bad = *status_of_row & RSD_ST_NAN_INPUT;
-        if (more) row = grad_row<T>(a, slot + rows);
-        const unsigned long long minus_m = tiles::both(f.none || f.plain ? 0.0f : -f.m), kk = tiles::both(a.k), minus_c = tiles::both(-f.c), c0 = tiles::both(f.c0), c1 = tiles::both(f.c1);
-        auto slope = [&](unsigned long long v, auto plain_row) {
-            float x, y;
-            const unsigned long long l = fma_f32x2(decltype(plain_row)::value ? v : add_f32x2(v, minus_m), kk, minus_c);
-            split_f32x2(l, x, y);
-            if (ENTROPY && !decltype(plain_row)::value) x = fmaxf(x, tiles::kFarBelow), y = fmaxf(y, tiles::kFarBelow);
-            const unsigned long long p = f32x2(ex2_approx(x), ex2_approx(y));
-            return tiles::mul_f32x2(p, ENTROPY ? fma_f32x2(f32x2(x, y), c1, c0) : c0);
-        };
-        const int head = ALIGNED ? 0 : (int)((uintptr_t)grad & 15u) / (int)sizeof(T);   // entries between the boundary and the gradient's first one
-        auto word = [&](int x, bool whole, auto plain_row) {
-            uint4 v = tiles::held_word<T, ALIGNED, kWords>(held, view, t0, t1, x, a.V);
-            if (bad) {
-                bool ignored = false;
-                P::clean(v, ignored);
-            }
-            if (ENTROPY && decltype(plain_row)::value) v = P::raised(v);
-            const uint4 g = P::make([&](int i) { return slope(P::pair(v, i), plain_row); });
-            if (whole || (x >= 0 && x + E <= a.V)) {
-                __stcs((uint4*)(grad + (int64_t)x * (int)sizeof(T)), g);
-            } else {
-                for (int i = 0; i < E; ++i)
-                    if (x + i >= 0 && x + i < a.V) P::store(grad, x + i, P::get(g, i));
-            }
-        };
-        auto write = [&](auto plain_row) {
-            const int last = t1 == n_tiles ? tiles::tiles_of<T>(head + a.V, kWords) : t1;   // tiles of the gradient: `head` entries ahead of the row's
-#pragma unroll 1
-            for (int t = t0 + warp; t < last && t0 < t1; t += NW) {
-                const int x = t * kTile - head + lane * E;
-                if (t * kTile >= head && (t + 1) * kTile - head <= a.V) {
-#pragma unroll 4
-                    for (int k = 0; k < kWords; ++k) word(x + k * 32 * E, true, plain_row);
-                } else {
-#pragma unroll 1
-                    for (int k = 0; k < kWords; ++k)
-                        if (x + k * 32 * E < a.V) word(x + k * 32 * E, false, plain_row);
-                }
-                __syncwarp();
-                // The entries of the tokens in this tile again, with their weights: a token given twice has both, and its first lane stores it.
-                const int32_t mine = lane < a.T ? tokens[lane] : -1;
-                if (mine >= 0 && (mine + head) / kTile == t) {
-                    float own = 0.0f;
-                    bool first = true;
-                    for (int i = 0; i < a.T; ++i)
-                        if (tokens[i] == mine) own += weights[i], first = first && i >= lane;
-                    if (first) {
-                        const int at = view.first + mine * (int)sizeof(T) - t0 * kWords * 512, tile = min(at / (kWords * 512), t1 - t0 - 1);
-                        float v = at >= 0 ? entry<T>(dynamic_bytes + at + tile * 16, 0) : entry<T>(view.base + view.first, mine), rest, ignored;
-                        if (decltype(plain_row)::value) v = fmaxf(v, tiles::kLow);
-                        split_f32x2(slope(tiles::both(v), plain_row), rest, ignored);
-                        P::store(grad, mine, f.none ? 0.0f : fmaf(own, f.inv_temp, rest));
-                    }
-                }
-                if (ALIGNED && more) {             // (a lane reads what it has fetched itself, and the tile's entries above)
-                    __syncwarp();
-                    fetch(row, t);
-                }
-            }
-        };
-        if (f.plain) write(std::true_type());
-        else write(std::false_type());
-        if (!more) break;
-        slot += rows;
-        if (!ALIGNED) {
-            __syncthreads();                       // (words of the gradient reach into other warps' tiles)
-            for (int t = t0 + warp; t < t1; t += NW) fetch(row, t);
+        for (int o = 16; o > 0; o >>= 1) G += __shfl_xor_sync(0xFFFFFFFFu, G, o);
+    }
+    tiles::row_barrier(blocks);
+    if (warp == 0) {
+        const Slope f = slope_of(join<ENTROPY>(sums, n_tiles, a.k, lane), G, h, a.inv_temp, a.k);
+        if (lane == 0) {
+            slope_of_row = f;
+            if (rank == 0) a.status[slot] = status_of_row | (f.none ? RSD_ST_EMPTY_ROW : 0);
         }
     }
+    __syncthreads();
+    const Slope f = slope_of_row;
+    bad = status_of_row & RSD_ST_NAN_INPUT;
+    char* const grad = (char*)a.grad + (int64_t)slot * a.V * (int64_t)sizeof(T);
+    const unsigned long long minus_m = tiles::both(f.none || f.plain ? 0.0f : -f.m), kk = tiles::both(a.k), minus_c = tiles::both(-f.c), c0 = tiles::both(f.c0), c1 = tiles::both(f.c1);
+    auto slope = [&](unsigned long long v, auto plain_row) {
+        float x, y;
+        const unsigned long long l = fma_f32x2(decltype(plain_row)::value ? v : add_f32x2(v, minus_m), kk, minus_c);
+        split_f32x2(l, x, y);
+        if (ENTROPY && !decltype(plain_row)::value) x = fmaxf(x, tiles::kFarBelow), y = fmaxf(y, tiles::kFarBelow);
+        const unsigned long long p = f32x2(ex2_approx(x), ex2_approx(y));
+        return tiles::mul_f32x2(p, ENTROPY ? fma_f32x2(f32x2(x, y), c1, c0) : c0);
+    };
+    const int head = ALIGNED ? 0 : (int)((uintptr_t)grad & 15u) / (int)sizeof(T);   // entries between the boundary and the gradient's first one
+    auto word = [&](uint4 v, auto plain_row) {
+        if (ENTROPY && decltype(plain_row)::value) v = P::raised(v);
+        return P::make([&](int i) { return slope(P::pair(v, i), plain_row); });
+    };
+    auto write = [&](auto plain_row) {
+        const int last = t1 == n_tiles ? tiles::tiles_of<T>(head + a.V, kWords) : t1;   // tiles of the gradient: `head` entries ahead of the row's
+#pragma unroll 1
+        for (int t = t0 + warp; t < last && t0 < t1; t += NW) {
+            const int x = t * kTile - head + lane * E;
+            char* const to = grad + (int64_t)x * (int)sizeof(T);
+            const bool whole = t * kTile >= head && (t + 1) * kTile - head <= a.V;
+            uint4 w[kWords];
+            tiles::held_words<T, ALIGNED, kWords>(w, held, view, t0, t1, x, a.V);
+            if (bad) {
+                bool ignored = false;
+#pragma unroll
+                for (int k = 0; k < kWords; ++k) P::clean(w[k], ignored);
+            }
+            if (whole) {
+#pragma unroll
+                for (int k = 0; k < kWords; ++k) __stcs((uint4*)(to + k * 512), word(w[k], plain_row));
+            } else {
+#pragma unroll
+                for (int k = 0; k < kWords; ++k) {
+                    const int at = x + k * 32 * E;
+                    if (at >= 0 && at + E <= a.V) {
+                        __stcs((uint4*)(to + k * 512), word(w[k], plain_row));
+                    } else if (at + E > 0 && at < a.V) {
+                        const uint4 g = word(w[k], plain_row);
+                        for (int i = 0; i < E; ++i)
+                            if (at + i >= 0 && at + i < a.V) P::store(grad, at + i, P::get(g, i));
+                    }
+                }
+            }
+            __syncwarp();
+            // The entries of the tokens in this tile again, with their weights: a token given twice has both, and its first lane stores it.
+            const int32_t mine = lane < a.T ? tokens[lane] : -1;
+            if (mine >= 0 && (mine + head) / kTile == t) {
+                float own = 0.0f;
+                bool first = true;
+                for (int i = 0; i < a.T; ++i)
+                    if (tokens[i] == mine) own += weights[i], first = first && i >= lane;
+                if (first) {
+                    const int at = view.first + mine * (int)sizeof(T) - t0 * kWords * 512, tile = min(at / (kWords * 512), t1 - t0 - 1);
+                    float v = at >= 0 ? entry<T>(dynamic_bytes + at + tile * 16, 0) : entry<T>(view.base + view.first, mine), rest, ignored;
+                    if (decltype(plain_row)::value) v = fmaxf(v, tiles::kLow);
+                    split_f32x2(slope(tiles::both(v), plain_row), rest, ignored);
+                    P::store(grad, mine, f.none ? 0.0f : fmaf(own, f.inv_temp, rest));
+                }
+            }
+        }
+    };
+    if (f.plain) write(std::true_type());
+    else write(std::false_type());
     grid_started();
 }
 

@@ -55,17 +55,12 @@ inline int holding_blocks(unsigned slots, int n_tiles, int tile_bytes, int warps
     while (blocks < tiles::kMaxBlocks && (n_tiles + blocks - 1) / blocks * tile_bytes > kHeldBytes) blocks *= 2;
     return blocks;
 }
-// Rows under way at a time where blocks take one after the other.
-inline unsigned rows_under_way(unsigned slots, int blocks, size_t smem, int warps) {
-    const int fit = std::max(1, std::min((int)(227 * 1024 / (smem + 1280)), 32 / warps));   // blocks on an SM (1280: static words and what a block costs)
-    return std::min(slots, (unsigned)std::max(1, rsd_host::sm_count() * fit / blocks));
-}
 template <typename T, bool ALIGNED, bool ENTROPY, int NW>
 void launch_score_grad_as(unsigned slots, int blocks, const ScoreArgs& a, cudaStream_t s) {
     const int n_tiles = tiles::tiles_of<T>(a.V, score::kWords);
-    const size_t smem = (size_t)((n_tiles + blocks - 1) / blocks) * tiles::kHeldTile<score::kWords> + 2 * score::sums_bytes(n_tiles);
+    const size_t smem = (size_t)((n_tiles + blocks - 1) / blocks) * tiles::kHeldTile<score::kWords> + score::sums_bytes(n_tiles);
     if (!rsd_host::raise_shared_memory<score::score_grad_kernel<T, ALIGNED, ENTROPY, NW>>(kMostHeldBytes)) return;
-    launch_rows(score::score_grad_kernel<T, ALIGNED, ENTROPY, NW>, rows_under_way(slots, blocks, smem, NW), blocks, NW * 32, smem, s, a);
+    launch_rows(score::score_grad_kernel<T, ALIGNED, ENTROPY, NW>, slots, blocks, NW * 32, smem, s, a);
 }
 template <typename T, bool ALIGNED, bool ENTROPY>
 void launch_score_grad_warps(unsigned slots, const ScoreArgs& a, cudaStream_t s) {
