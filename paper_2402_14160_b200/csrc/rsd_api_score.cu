@@ -120,7 +120,6 @@ int rsd_token_logprobs_backward(const rsd_rows* rows, int B, int R, int V, const
     a.num_rows = R; a.token = token; a.g_logprob = grad_logprob; a.g_entropy = grad_entropy; a.grad = grad_rows; a.status = status;
     const bool aligned = rows_aligned(rows) && dense_aligned(grad_rows, V, rows->dtype);
     const unsigned slots = (unsigned)((int64_t)B * R);
-    a.slots = (int)slots;
     if (rows->dtype == RSD_F32) rsd::launch_score_grad_f32(aligned, slots, a, s);
     else rsd::launch_score_grad_bf16(aligned, slots, a, s);
     return check_launch("rsd_token_logprobs_backward");
@@ -153,7 +152,6 @@ int rsd_row_divergence_backward(const rsd_rows* draft, const rsd_rows* target, i
     a.g_kl = grad_kl; a.g_reverse = grad_reverse_kl; a.grad = grad_draft; a.status = status;
     const bool aligned = rows_aligned(draft) && rows_aligned(target) && dense_aligned(grad_draft, V, draft->dtype);
     const unsigned slots = (unsigned)((int64_t)B * R);
-    a.slots = (int)slots;
     if (draft->dtype == RSD_F32) rsd::launch_divergence_grad_f32(aligned, slots, a, s);
     else rsd::launch_divergence_grad_bf16(aligned, slots, a, s);
     return check_launch("rsd_row_divergence_backward");

@@ -14,17 +14,15 @@ namespace rsd {
 
 namespace divergence {
 
-constexpr int kThreads = 256, kWarps = kThreads / 32, kWords = 4;
-constexpr int kMaxTiles = RSD_MAX_VOCAB / tiles::tile_entries<float>(kWords);
+constexpr int kWords = 4;
 
-struct Sums {   // of the rows' tiles, relative to each tile's largest entries; every block of the pair has all of them
-    float mp[kMaxTiles], mq[kMaxTiles], sp[kMaxTiles], sq[kMaxTiles], dp[kMaxTiles], dq[kMaxTiles];
+struct Sums {   // of a tile of both rows, relative to its largest entries; every block of the pair has those of all tiles
+    float sp, sq, dp, dq, mp, mq, overlap, unused;
 };
 struct Totals {
-    float mp, mq, sp, sq, dp, dq;   // largest entries, sums of weights, of weight times b - a (p), a - b (q)
+    float sp, sq, dp, dq, mp, mq;   // sums of weights, of weight times b - a (p), a - b (q), largest entries
 };
 struct Smem {
-    Sums sums;
     Totals total;
     uint32_t alone_p, alone_q;      // largest entry whose token the other row lacks, as an ordered word (0: none)
     int status;
@@ -89,9 +87,10 @@ __device__ __noinline__ CarefulSums add_tile_careful(Words p, Words q, float mp,
     return l;
 }
 
+// masked: the row's last tile had entries without mass, so that this one is looked through for them at once.
 template <typename T, bool BOTH>   // BOTH: the sums of weight times difference too
-__device__ __forceinline__ void tile_sums(uint4 (&p)[kWords], uint4 (&q)[kWords], float kp, float kq, int t, int lane, uint32_t blocks, Smem& sm, float& alone_p, float& alone_q,
-                                          bool& bad) {
+__device__ __forceinline__ void tile_sums(uint4 (&p)[kWords], uint4 (&q)[kWords], float kp, float kq, int t, int lane, uint32_t blocks, Sums* sums, float& alone_p, float& alone_q,
+                                          bool& bad, bool& masked) {
     using P = tiles::Packed16<T>;
     float mp = tiles::warp_max_nan(P::largest(p)), mq = tiles::warp_max_nan(P::largest(q));
     if (!(mp < __builtin_huge_valf()) || !(mq < __builtin_huge_valf())) {   // NaN or +inf: no entries
@@ -101,13 +100,26 @@ __device__ __forceinline__ void tile_sums(uint4 (&p)[kWords], uint4 (&q)[kWords]
     }
     LaneSums l = {tiles::both(0.0f), tiles::both(0.0f), tiles::both(0.0f), tiles::both(0.0f)};
     const bool plain = tiles::plain_tile(mp, kp) && tiles::plain_tile(mq, kq);
-    if (plain && (!BOTH || __all_sync(0xFFFFFFFFu, fminf(P::smallest(p), P::smallest(q)) > tiles::kLow))) {
+    float x, y, sp, sq, dp, dq;
+    auto halves = [&] {
+        split_f32x2(l.sp, x, y), sp = x + y;
+        split_f32x2(l.sq, x, y), sq = x + y;
+        split_f32x2(l.dp, x, y), dp = -(x + y);
+        split_f32x2(l.dq, x, y), dq = x + y;
+    };
+    bool done = false;
+    if (plain && !(BOTH && masked)) {
         add_tile<T, BOTH, false>(p, q, mp, mq, kp, kq, l);
-    } else {
+        halves();
+        done = !BOTH || !__any_sync(0xFFFFFFFFu, !(fabsf(dp + dq) < __builtin_huge_valf()));   // (an entry without mass gives 0 times infinity)
+    }
+    if (!done) {
+        masked = true;
         bool alike = true;
 #pragma unroll
         for (int i = 0; i < kWords; ++i) alike = alike && !P::differ(p[i], q[i]);
         if (BOTH && plain && __all_sync(0xFFFFFFFFu, alike)) {
+            l = {tiles::both(0.0f), tiles::both(0.0f), tiles::both(0.0f), tiles::both(0.0f)};
             add_tile<T, BOTH, true>(p, q, mp, mq, kp, kq, l);
         } else {
             Words pw, qw;
@@ -117,65 +129,53 @@ __device__ __forceinline__ void tile_sums(uint4 (&p)[kWords], uint4 (&q)[kWords]
             l = {f32x2(c.sp, 0.0f), f32x2(c.sq, 0.0f), f32x2(c.dp, 0.0f), f32x2(c.dq, 0.0f)};
             alone_p = fmaxf(alone_p, c.alone_p), alone_q = fmaxf(alone_q, c.alone_q);
         }
+        halves();
     }
-    float x, y;
-    split_f32x2(l.sp, x, y);
-    const float sp = x + y;
-    split_f32x2(l.sq, x, y);
-    const float sq = x + y;
-    split_f32x2(l.dp, x, y);
-    const float dp = -(x + y);
-    split_f32x2(l.dq, x, y);
-    const float dq = x + y;
-    const uint32_t to = lane & 7;
-    if (BOTH) {
-        const float sum = tiles::warp_sum_four(sp, sq, dp, dq, lane);   // eight lanes each
-        if (to < blocks) {
-            float* const at = lane < 8 ? sm.sums.sp : lane < 16 ? sm.sums.sq : lane < 24 ? sm.sums.dp : sm.sums.dq;
-            tiles::store_at(at + t, to, sum);
-            if (lane < 16) tiles::store_at((lane < 8 ? sm.sums.mp : sm.sums.mq) + t, to, lane < 8 ? mp : mq);
-        }
+    // Sums::sp, sq, dp, dq are in eight lanes each (without the last two in sixteen each); four lanes store them and two the largest entries, in every block.
+    const float sum = BOTH ? tiles::warp_sum_four(sp, sq, dp, dq, lane) : tiles::warp_sum_two(sp, sq, lane);
+    const int member = (lane & 4) ? 4 + (lane >> 4) : BOTH ? lane >> 3 : lane >> 4;
+    const float value = (lane & 4) ? (lane < 16 ? mp : mq) : sum;
+    float* const to = (float*)&sums[t] + member;
+    if (blocks == 1) {
+        if ((lane & 3) == 0) *to = value;          // (several lanes store the same)
     } else {
-        const float sum = tiles::warp_sum_two(sp, sq, lane);            // sixteen lanes each
-        if (to < blocks) {
-            float* const at = lane < 8 ? sm.sums.sp : lane < 16 ? sm.sums.mp : lane < 24 ? sm.sums.sq : sm.sums.mq;
-            tiles::store_at(at + t, to, lane < 8 || (lane >= 16 && lane < 24) ? sum : lane < 16 ? mp : mq);
-        }
+        for (uint32_t r = lane & 3; r < blocks; r += 4) tiles::store_at(to, r, value);
     }
 }
 
 // The tiles' sums joined by one warp; every lane gets the result.
 template <bool BOTH>
-__device__ __forceinline__ Totals join(const Sums& sums, int n, float kp, float kq, int lane) {
+__device__ __forceinline__ Totals join(const Sums* sums, int n, float kp, float kq, int lane) {
     float mp = kNegInf, mq = kNegInf;
-    for (int t = lane; t < n; t += 32) mp = fmaxf(mp, sums.mp[t]), mq = fmaxf(mq, sums.mq[t]);
-    mp = warp_max(mp), mq = warp_max(mq);
+    for (int t = lane; t < n; t += 32) mp = fmaxf(mp, sums[t].mp), mq = fmaxf(mq, sums[t].mq);
+    mp = tiles::warp_max_nan(mp), mq = tiles::warp_max_nan(mq);
     float sp = 0.0f, sq = 0.0f, dp = 0.0f, dq = 0.0f;
     for (int t = lane; t < n; t += 32) {
-        const float mtp = sums.mp[t], mtq = sums.mq[t];
+        const float mtp = sums[t].mp, mtq = sums[t].mq;
         const bool has_p = mtp > kNegInf, has_q = mtq > kNegInf;
         const float bp = has_p ? fmaxf((mtp - mp) * kp, tiles::kFarBelow) - tiles::rounded_off(mtp, kp) : 0.0f;
         const float bq = has_q ? fmaxf((mtq - mq) * kq, tiles::kFarBelow) - tiles::rounded_off(mtq, kq) : 0.0f;
         const float fp = has_p ? ex2_approx(bp) : 0.0f, fq = has_q ? ex2_approx(bq) : 0.0f;
-        sp = fmaf(fp, sums.sp[t], sp), sq = fmaf(fq, sums.sq[t], sq);
+        sp = fmaf(fp, sums[t].sp, sp), sq = fmaf(fq, sums[t].sq, sq);
         if (BOTH) {
             const float d = has_p && has_q ? bq - bp : 0.0f;
-            dp = fmaf(fp, fmaf(-d, sums.sp[t], sums.dp[t]), dp), dq = fmaf(fq, fmaf(d, sums.sq[t], sums.dq[t]), dq);
+            dp = fmaf(fp, fmaf(-d, sums[t].sp, sums[t].dp), dp), dq = fmaf(fq, fmaf(d, sums[t].sq, sums[t].dq), dq);
         }
     }
     const float sum = tiles::warp_sum_four(sp, sq, dp, dq, lane);
-    return {mp, mq, __shfl_sync(0xFFFFFFFFu, sum, 0), __shfl_sync(0xFFFFFFFFu, sum, 8), __shfl_sync(0xFFFFFFFFu, sum, 16), __shfl_sync(0xFFFFFFFFu, sum, 24)};
+    return {__shfl_sync(0xFFFFFFFFu, sum, 0), __shfl_sync(0xFFFFFFFFu, sum, 8), __shfl_sync(0xFFFFFFFFu, sum, 16), __shfl_sync(0xFFFFFFFFu, sum, 24), mp, mq};
 }
 
-// A pair of rows and the tiles of it that this warp has: tile t belongs to warp t / blocks mod kWarps of block t mod blocks.
+// A pair of rows and the tiles of it that this warp has: tile t belongs to warp t / blocks mod NW of block t mod blocks.
 struct Pair {
     tiles::View draft, target;
     int64_t slot;
     uint32_t rank, blocks;
     int n_tiles, first, step;
+    Sums* sums;
 };
-template <typename T>
-__device__ __forceinline__ Pair pair_of(const DivergenceArgs& a) {
+template <typename T, int NW>
+__device__ __forceinline__ Pair pair_of(const DivergenceArgs& a, unsigned char* dynamic_bytes) {
     Pair w;
     w.rank = tiles::cluster_rank(), w.blocks = tiles::cluster_blocks();
     const uint32_t slot = blockIdx.x / w.blocks, sequence = slot / (uint32_t)a.R;
@@ -185,26 +185,28 @@ __device__ __forceinline__ Pair pair_of(const DivergenceArgs& a) {
     w.draft = tiles::view_of<T>((const T*)a.draft + b * a.draft_seq + r * a.draft_row, a.V);
     w.target = tiles::view_of<T>((const T*)a.target + b * a.target_seq + r * a.target_row, a.V);
     w.n_tiles = tiles::tiles_of<T>(a.V, kWords);
-    w.first = (int)(threadIdx.x >> 5) * (int)w.blocks + (int)w.rank, w.step = kWarps * (int)w.blocks;
+    w.first = (int)(threadIdx.x >> 5) * (int)w.blocks + (int)w.rank, w.step = NW * (int)w.blocks;
+    w.sums = (Sums*)dynamic_bytes;
     return w;
 }
 
 // Both rows, read into the tiles' sums; everything else of a pair follows from what this leaves in every block's shared memory.  True: there were NaN or +inf.
-template <typename T, bool ALIGNED, bool BOTH>
+template <typename T, bool ALIGNED, bool BOTH, int NW>
 __device__ __forceinline__ bool read_rows(const DivergenceArgs& a, const Pair& w, Smem& sm) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     if (threadIdx.x == 0) sm.status = 0, sm.alone_p = sm.alone_q = 0;
     if (w.blocks > 1) tiles::cluster_arrive();     // (the pair's other blocks have started, and their words above are set, behind the wait below)
+    else __syncthreads();
     grid_wait();
     if (w.blocks > 1) tiles::cluster_wait();
-    else __syncthreads();
     float alone_p = kNegInf, alone_q = kNegInf;
-    bool bad = false;
+    bool bad = false, masked = false;
+#pragma unroll 1
     for (int t = w.first; t < w.n_tiles; t += w.step) {
         uint4 p[kWords], q[kWords];
         tiles::load_tile<T, ALIGNED, kWords>(p, w.draft, t, lane, a.V);
         tiles::load_tile<T, ALIGNED, kWords>(q, w.target, t, lane, a.V);
-        tile_sums<T, BOTH>(p, q, a.k_draft, a.k_target, t, lane, w.blocks, sm, alone_p, alone_q, bad);
+        tile_sums<T, BOTH>(p, q, a.k_draft, a.k_target, t, lane, w.blocks, w.sums, alone_p, alone_q, bad, masked);
     }
     if (bad || alone_p > kNegInf || alone_q > kNegInf)
         for (uint32_t i = 0; i < w.blocks; ++i) {
@@ -214,7 +216,7 @@ __device__ __forceinline__ bool read_rows(const DivergenceArgs& a, const Pair& w
         }
     tiles::row_barrier(w.blocks);
     if (warp == 0) {
-        const Totals t = join<BOTH>(sm.sums, w.n_tiles, a.k_draft, a.k_target, lane);
+        const Totals t = join<BOTH>(w.sums, w.n_tiles, a.k_draft, a.k_target, lane);
         if (lane == 0) sm.total = t;
     }
     __syncthreads();
@@ -258,19 +260,20 @@ struct LogProb {
 __device__ __forceinline__ LogProb log_prob(float m, float k, float log2s, bool empty) {
     LogProb l;
     l.plain = tiles::plain_tile(m, k);
-    const double exact = l.plain ? (double)m * (double)k + (double)log2s : (double)log2s;
-    l.c = (float)exact, l.off = (float)((double)l.c - exact);
+    l.c = l.plain ? fmaf(m, k, log2s) : log2s;
+    l.off = l.plain ? -(fmaf(m, k, -l.c) + log2s) : 0.0f;
     l.kk = tiles::both(k), l.minus_c = tiles::both(-l.c), l.minus_m = tiles::both(l.plain || empty ? 0.0f : -m);
     return l;
 }
 
-template <typename T, bool ALIGNED>
-__global__ void __launch_bounds__(kThreads, 3) divergence_kernel(const __grid_constant__ DivergenceArgs a) {
+template <typename T, bool ALIGNED, int NW>
+__global__ void __launch_bounds__(NW * 32, 24 / NW) divergence_kernel(const __grid_constant__ DivergenceArgs a) {
     using P = tiles::Packed16<T>;
+    extern __shared__ __align__(16) unsigned char dynamic_bytes[];   // all tiles' sums
     __shared__ Smem sm;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const Pair w = pair_of<T>(a);
-    const bool bad = read_rows<T, ALIGNED, true>(a, w, sm);
+    const Pair w = pair_of<T, NW>(a, dynamic_bytes);
+    const bool bad = read_rows<T, ALIGNED, true, NW>(a, w, sm);
     const Result res = result_of(a, sm);
     if (w.rank == 0 && tid == 0) {
         const Totals& t = sm.total;
@@ -282,10 +285,9 @@ __global__ void __launch_bounds__(kThreads, 3) divergence_kernel(const __grid_co
     if (a.out_overlap) {
         const LogProb p = log_prob(sm.total.mp, a.k_draft, res.log2_sp, res.empty), q = log_prob(sm.total.mq, a.k_target, res.log2_sq, res.empty);
         const unsigned long long shift = tiles::both(q.off - p.off);
-        const float scale = exp2f(p.off);
-        tiles::row_barrier(w.blocks);                               // (the tiles' sums are read no more: the overlaps take the place of mp)
         auto sweep = [&](auto plain) {
             constexpr bool PLAIN = decltype(plain)::value;
+#pragma unroll 1
             for (int t = w.first; t < w.n_tiles; t += w.step) {
                 uint4 pw[kWords], qw[kWords];
                 tiles::load_tile<T, ALIGNED, kWords>(pw, w.draft, t, lane, a.V);
@@ -308,7 +310,7 @@ __global__ void __launch_bounds__(kThreads, 3) divergence_kernel(const __grid_co
                 float x, y;
                 split_f32x2(s, x, y);
                 const float sum = tiles::warp_sum_two(x + y, 0.0f, lane);
-                if (lane == 0) tiles::store_at(&sm.sums.mp[t], 0, sum);
+                if (lane == 0) tiles::store_at(&w.sums[t].overlap, 0, sum);
             }
         };
         if (!res.empty) {
@@ -318,69 +320,77 @@ __global__ void __launch_bounds__(kThreads, 3) divergence_kernel(const __grid_co
         tiles::row_barrier(w.blocks);
         if (w.rank == 0 && warp == 0) {
             float s = 0.0f;
-            for (int t = lane; t < w.n_tiles; t += 32) s += sm.sums.mp[t];
+            for (int t = lane; t < w.n_tiles; t += 32) s += w.sums[t].overlap;
             s = tiles::warp_sum_two(s, 0.0f, lane);
-            if (lane == 0) a.out_overlap[w.slot] = res.empty ? 0.0f : fminf(s * scale, 1.0f);
+            if (lane == 0) a.out_overlap[w.slot] = res.empty ? 0.0f : fminf(s * ex2_approx(p.off), 1.0f);
         }
     }
     grid_started();
 }
 
 // d KL(q||p) / dv_x = (p_x - q_x) / T,   d KL(p||q) / dv_x = p_x (log p_x - log q_x - KL(p||q)) / T,   v the draft row, T its temperature.
-// A row whose KL(p||q) is infinite has no gradient of it.  The rows are read twice, the second time from L2.
-template <typename T, bool ALIGNED, bool REVERSE>
-__global__ void __launch_bounds__(kThreads, 3) divergence_grad_kernel(const __grid_constant__ DivergenceArgs a) {
+// A row whose KL(p||q) is infinite has no gradient of it.  Words of the gradient are written on their own 16-byte boundaries.
+template <typename T, bool ALIGNED, bool REVERSE, int NW>
+__global__ void __launch_bounds__(NW * 32, 24 / NW) divergence_grad_kernel(const __grid_constant__ DivergenceArgs a) {
     using P = tiles::Packed16<T>;
-    constexpr int E = P::kEntries;
+    constexpr int E = P::kEntries, kTile = tiles::tile_entries<T>(kWords);
+    extern __shared__ __align__(16) unsigned char dynamic_bytes[];   // all tiles' sums
     __shared__ Smem sm;
     const int tid = threadIdx.x, lane = tid & 31;
-    const Pair w = pair_of<T>(a);
-    char* grad = (char*)a.grad + w.slot * a.V * (int64_t)sizeof(T);
-    const bool bad = read_rows<T, ALIGNED, REVERSE>(a, w, sm);
-    const Result res = result_of(a, sm);
+    const Pair w = pair_of<T, NW>(a, dynamic_bytes);
+    const bool bad = read_rows<T, ALIGNED, REVERSE, NW>(a, w, sm);
     const float g = a.g_kl ? a.g_kl[w.slot] : 0.0f, h = REVERSE ? a.g_reverse[w.slot] : 0.0f;
-    const float inv_temp = a.inv_draft_temp, gt = res.empty ? 0.0f : g * inv_temp, ht = res.empty || (REVERSE && res.reverse_infinite) ? 0.0f : h * inv_temp;
+    const Result res = result_of(a, sm);
+    const float gt = res.empty ? 0.0f : g * a.inv_draft_temp, ht = res.empty || (REVERSE && res.reverse_infinite) ? 0.0f : h * a.inv_draft_temp;
     const LogProb lp = log_prob(sm.total.mp, a.k_draft, res.log2_sp, res.empty), lq = log_prob(sm.total.mq, a.k_target, res.log2_sq, res.empty);
-    const float scale_p = exp2f(lp.off), scale_q = exp2f(lq.off);
+    const float scale_p = ex2_approx(lp.off), scale_q = ex2_approx(lq.off);
     // gt (p - q) + p ht (ln 2 (log2 p - log2 q) - KL(p||q)); rows that are equal give 0
-    const float reverse = ht != 0.0f ? 0.69314718f * (sm.total.dp / sm.total.sp + log2f(sm.total.sq / sm.total.sp)) : 0.0f;
+    const float reverse = REVERSE && ht != 0.0f ? 0.69314718f * (__fdividef(sm.total.dp, sm.total.sp) + res.log2_sq - res.log2_sp) : 0.0f;
     const float c1f = ht * 0.69314718f, c0f = fmaf(c1f, lp.off - lq.off, -ht * reverse);
-    const unsigned long long c0 = tiles::both(c0f * scale_p), c1 = tiles::both(c1f * scale_p), cg = tiles::both(gt * scale_p), minus_ratio = tiles::both(-(scale_q / scale_p)),
+    const unsigned long long c0 = tiles::both(c0f * scale_p), c1 = tiles::both(c1f * scale_p), cg = tiles::both(gt * scale_p), minus_ratio = tiles::both(-__fdividef(scale_q, scale_p)),
                              minus_one = tiles::both(-1.0f);
-    const int head = (int)((uintptr_t)grad & 15u) / (int)sizeof(T);
-    const int out_tiles = tiles::tiles_of<T>(head + a.V, kWords);
-    auto write = [&](auto plain) {
+    char* const grad = (char*)a.grad + w.slot * a.V * (int64_t)sizeof(T);
+    const int head = ALIGNED ? 0 : (int)((uintptr_t)grad & 15u) / (int)sizeof(T);   // entries between the boundary and the gradient's first one
+    auto word = [&](uint4 pw, uint4 qw, auto plain) {
         constexpr bool PLAIN = decltype(plain)::value;
-        for (int t = w.first; t < out_tiles; t += w.step) {
-            const int x0 = t * tiles::tile_entries<T>(kWords) + lane * E - head, from = x0 - lane * E;
-            const bool whole = from >= 0 && from + tiles::tile_entries<T>(kWords) <= a.V;
+        if (REVERSE && PLAIN) pw = P::raised(pw), qw = P::raised(qw);
+        return P::make([&](int i) {
+            float x, y, u, v;
+            split_f32x2(lp.of<PLAIN>(P::pair(pw, i)), x, y);
+            split_f32x2(lq.of<PLAIN>(P::pair(qw, i)), u, v);
+            const unsigned long long wp = f32x2(ex2_approx(x), ex2_approx(y)), wq = f32x2(ex2_approx(u), ex2_approx(v));
+            const unsigned long long apart = tiles::mul_f32x2(fma_f32x2(wq, minus_ratio, wp), cg);
+            if (!REVERSE) return apart;
+            if (!PLAIN) x = fmaxf(x, tiles::kFarBelow), y = fmaxf(y, tiles::kFarBelow), u = fmaxf(u, tiles::kFarBelow), v = fmaxf(v, tiles::kFarBelow);
+            return fma_f32x2(wp, fma_f32x2(fma_f32x2(f32x2(u, v), minus_one, f32x2(x, y)), c1, c0), apart);
+        });
+    };
+    auto write = [&](auto plain) {
+        const int last = tiles::tiles_of<T>(head + a.V, kWords);    // tiles of the gradient: `head` entries ahead of the rows'
+#pragma unroll 1
+        for (int t = w.first; t < last; t += w.step) {
+            const int x = t * kTile - head + lane * E;
+            char* const to = grad + (int64_t)x * (int)sizeof(T);
+            const bool whole = t * kTile >= head && (t + 1) * kTile - head <= a.V;
             uint4 pw[kWords], qw[kWords];
-            tiles::load_words<T, ALIGNED, kWords>(pw, w.draft, x0, whole, a.V);
-            tiles::load_words<T, ALIGNED, kWords>(qw, w.target, x0, whole, a.V);
+            tiles::load_words<T, ALIGNED, kWords>(pw, w.draft, x, whole, a.V);
+            tiles::load_words<T, ALIGNED, kWords>(qw, w.target, x, whole, a.V);
+            if (bad) {
+                bool ignored = false;
+#pragma unroll
+                for (int k = 0; k < kWords; ++k) P::clean(pw[k], ignored), P::clean(qw[k], ignored);
+            }
 #pragma unroll
             for (int k = 0; k < kWords; ++k) {
-                if (bad) {
-                    bool ignored = false;
-                    P::clean(pw[k], ignored), P::clean(qw[k], ignored);
-                }
-                const uint4 pr = REVERSE && PLAIN ? P::raised(pw[k]) : pw[k], qr = REVERSE && PLAIN ? P::raised(qw[k]) : qw[k];
-                uint4 out = P::make([&](int i) {
-                    float x, y, u, v;
-                    split_f32x2(lp.of<PLAIN>(P::pair(pr, i)), x, y);
-                    split_f32x2(lq.of<PLAIN>(P::pair(qr, i)), u, v);
-                    const unsigned long long wp = f32x2(ex2_approx(x), ex2_approx(y)), wq = f32x2(ex2_approx(u), ex2_approx(v));
-                    const unsigned long long apart = tiles::mul_f32x2(fma_f32x2(wq, minus_ratio, wp), cg);
-                    if (!REVERSE) return apart;
-                    if (!PLAIN) x = fmaxf(x, tiles::kFarBelow), y = fmaxf(y, tiles::kFarBelow), u = fmaxf(u, tiles::kFarBelow), v = fmaxf(v, tiles::kFarBelow);
-                    return fma_f32x2(wp, fma_f32x2(fma_f32x2(f32x2(u, v), minus_one, f32x2(x, y)), c1, c0), apart);
-                });
-                const int x = x0 + k * 32 * E;
+                const int at = x + k * 32 * E;
+                if (!whole && (at >= a.V || at + E <= 0)) continue;
+                uint4 out = word(pw[k], qw[k], plain);
                 if (res.empty) out = make_uint4(0, 0, 0, 0);
-                if (whole || (x >= 0 && x + E <= a.V)) {
-                    *(uint4*)(grad + (int64_t)x * (int)sizeof(T)) = out;
+                if (whole || (at >= 0 && at + E <= a.V)) {
+                    __stcs((uint4*)(to + k * 512), out);
                 } else {
                     for (int i = 0; i < E; ++i)
-                        if (x + i >= 0 && x + i < a.V) P::store(grad, x + i, P::get(out, i));
+                        if (at + i >= 0 && at + i < a.V) P::store(grad, at + i, P::get(out, i));
                 }
             }
         }

@@ -32,7 +32,6 @@ struct DivergenceArgs {
     int32_t* status;
     const float *g_kl, *g_reverse;
     void* grad;
-    int slots;
 };
 
 // `slots` rows (or pairs of rows), a block or a cluster of blocks each.  aligned: rows (and gradient rows) start on 16-byte boundaries.

@@ -80,17 +80,34 @@ void launch_score_grad_of(bool aligned, unsigned slots, const ScoreArgs& a, cuda
         else launch_score_grad_warps<T, false, false>(slots, a, s);
     }
 }
+template <typename T, bool ALIGNED, int NW>
+void launch_divergence_as(unsigned slots, const DivergenceArgs& a, cudaStream_t s) {
+    namespace d = divergence;
+    const int n_tiles = tiles::tiles_of<T>(a.V, d::kWords), blocks = env_int("GB", 0) ? env_int("GB", 0) : row_blocks(slots, n_tiles, NW);
+    launch_rows(d::divergence_kernel<T, ALIGNED, NW>, slots, blocks, NW * 32, (size_t)n_tiles * sizeof(d::Sums), s, a);
+}
 template <typename T>
 void launch_divergence_of(bool aligned, unsigned slots, const DivergenceArgs& a, cudaStream_t s) {
-    const int blocks = row_blocks(slots, tiles::tiles_of<T>(a.V, divergence::kWords), divergence::kWarps);
-    launch_rows(aligned ? divergence::divergence_kernel<T, true> : divergence::divergence_kernel<T, false>, slots, blocks, divergence::kThreads, 0, s, a);
+    const int nw = env_int("NW", 8);
+    if (aligned) nw == 8 ? launch_divergence_as<T, true, 8>(slots, a, s) : launch_divergence_as<T, true, 4>(slots, a, s);
+    else nw == 8 ? launch_divergence_as<T, false, 8>(slots, a, s) : launch_divergence_as<T, false, 4>(slots, a, s);
+}
+template <typename T, bool ALIGNED, bool REVERSE, int NW>
+void launch_divergence_grad_as(unsigned slots, const DivergenceArgs& a, cudaStream_t s) {
+    namespace d = divergence;
+    const int n_tiles = tiles::tiles_of<T>(a.V, d::kWords), blocks = env_int("GB", 0) ? env_int("GB", 0) : row_blocks(slots, n_tiles, NW);
+    launch_rows(d::divergence_grad_kernel<T, ALIGNED, REVERSE, NW>, slots, blocks, NW * 32, (size_t)n_tiles * sizeof(d::Sums), s, a);
+}
+template <typename T, bool REVERSE>
+void launch_divergence_grad_warps(bool aligned, unsigned slots, const DivergenceArgs& a, cudaStream_t s) {
+    const int nw = env_int("NW", 8);
+    if (aligned) nw == 8 ? launch_divergence_grad_as<T, true, REVERSE, 8>(slots, a, s) : launch_divergence_grad_as<T, true, REVERSE, 4>(slots, a, s);
+    else nw == 8 ? launch_divergence_grad_as<T, false, REVERSE, 8>(slots, a, s) : launch_divergence_grad_as<T, false, REVERSE, 4>(slots, a, s);
 }
 template <typename T>
 void launch_divergence_grad_of(bool aligned, unsigned slots, const DivergenceArgs& a, cudaStream_t s) {
-    namespace d = divergence;
-    const int blocks = row_blocks(slots, tiles::tiles_of<T>(a.V, d::kWords), d::kWarps);
-    if (a.g_reverse) launch_rows(aligned ? d::divergence_grad_kernel<T, true, true> : d::divergence_grad_kernel<T, false, true>, slots, blocks, d::kThreads, 0, s, a);
-    else launch_rows(aligned ? d::divergence_grad_kernel<T, true, false> : d::divergence_grad_kernel<T, false, false>, slots, blocks, d::kThreads, 0, s, a);
+    if (a.g_reverse) launch_divergence_grad_warps<T, true>(aligned, slots, a, s);
+    else launch_divergence_grad_warps<T, false>(aligned, slots, a, s);
 }
 
 }  // namespace rsd
