@@ -267,7 +267,7 @@ __device__ __forceinline__ LogProb log_prob(float m, float k, float log2s, bool 
 }
 
 template <typename T, bool ALIGNED, int NW>
-__global__ void __launch_bounds__(NW * 32, 24 / NW) divergence_kernel(const __grid_constant__ DivergenceArgs a) {
+__global__ void __launch_bounds__(NW * 32, 32 / NW) divergence_kernel(const __grid_constant__ DivergenceArgs a) {
     using P = tiles::Packed16<T>;
     extern __shared__ __align__(16) unsigned char dynamic_bytes[];   // all tiles' sums
     __shared__ Smem sm;
