@@ -128,29 +128,36 @@ __device__ __forceinline__ float entry(const void* row, int x) {   // -inf where
 
 // ---- the K largest entries of a row ----------------------------------------------------------------------------------------------
 // Every lane knows its largest entry of each tile (a group of up to 64 entries).  The largest of a block's even and of its odd tiles in each lane are
-// kBuckets distinct entries: the K-th largest of them is at most the K-th largest entry of the row, and so is the largest such bound of
-// the row's blocks.  Only groups that reach it are read again (they lie in L2), a word a thread, and only entries that reach it are
-// ranked: about 1.4 K of them.
+// kBuckets distinct entries: the K-th largest of them is at most the K-th largest entry of the block's tiles.  Only groups that reach that bound are read again
+// (they lie in L2), a word a thread; the entries that reach it, about 1.4 K of a block, go to the row's first block, which ranks those that reach
+// the largest of the blocks' bounds.
 template <int NW>
 struct TopSmem {
     float bucket[NW][kBuckets];
-    float bound[tiles::kMaxBlocks];   // of every block of the row
+    float bound, bounds[tiles::kMaxBlocks];   // the block's; in the first block those of all
     int32_t group[kList];
-    float all_value[kList];           // in the first block: the entries of all
-    int32_t all_token[kList];
-    int groups, all_count, overflow;
+    unsigned long long key[kList];            // in the first block: the entries of all, by value, then by token (the smaller one is larger)
+    int groups, count, kept, overflow;
     float best_value[NW];
     int best_token[NW];
 };
+__device__ __forceinline__ unsigned long long key_of(float v, int x) { return (unsigned long long)float_to_ordered(v + 0.0f) << 32 | (uint32_t)~x; }   // (-0 is 0)
+__device__ __forceinline__ float value_of(unsigned long long key) { return ordered_to_float((uint32_t)(key >> 32)); }
+__device__ __forceinline__ int token_of(unsigned long long key) { return (int)~(uint32_t)key; }
 
-// K-th largest of 64 values, two per lane, from below: exact in its upper 16 bits.
+// K-th largest of 64 values, two per lane, from below: exact in its upper 16 bits, found two bits at a time.
 __device__ __forceinline__ float bound_of_kth(float a, float b, int K) {
     const uint32_t ca = a > kNegInf ? float_to_ordered(a) >> 16 : 0u, cb = b > kNegInf ? float_to_ordered(b) >> 16 : 0u;
     uint32_t code = 0;
 #pragma unroll 1
-    for (uint32_t bit = 0x8000u; bit; bit >>= 1) {
-        const uint32_t c = code | bit;
-        if (__popc(__ballot_sync(0xFFFFFFFFu, ca >= c)) + __popc(__ballot_sync(0xFFFFFFFFu, cb >= c)) >= K) code = c;
+    for (int at = 14; at >= 0; at -= 2) {
+        int reached = 0;
+#pragma unroll
+        for (uint32_t i = 1; i < 4; ++i) {
+            const uint32_t c = code | i << at;
+            reached += __popc(__ballot_sync(0xFFFFFFFFu, ca >= c)) + __popc(__ballot_sync(0xFFFFFFFFu, cb >= c)) >= K;
+        }
+        code |= (uint32_t)reached << at;
     }
     return code ? ordered_to_float(code << 16) : kNegInf;      // (fewer than K buckets hold an entry: no bound)
 }
@@ -181,36 +188,31 @@ __device__ __noinline__ void top_one_by_one(const void* row, int V, int K, TopSm
             if (sm.best_token[j] >= 0 && (at < 0 || sm.best_value[j] > v || (sm.best_value[j] == v && sm.best_token[j] < at))) v = sm.best_value[j], at = sm.best_token[j];
         if (at < 0) break;
         last_v = v, last_x = at;
-        if (threadIdx.x == 0) sm.all_value[found] = v, sm.all_token[found] = at;
+        if (threadIdx.x == 0) sm.key[found] = key_of(v, at);
     }
     __syncthreads();
-    if (threadIdx.x == 0) sm.all_count = found;
+    if (threadIdx.x == 0) sm.count = found;
     __syncthreads();
 }
 
-// Bound of a block, known to all blocks of the row behind the next barrier.  even, odd: the lane's largest entries.
-template <int NW>
-__device__ __forceinline__ void block_bound(TopSmem<NW>& sm, float even, float odd, int K, uint32_t rank, uint32_t blocks) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    if (NW > 1) {
-        sm.bucket[warp][lane] = even, sm.bucket[warp][lane + 32] = odd;
-        __syncthreads();
-    }
+// The entries of the block's tiles that reach its bound, in the first block's list.  even, odd: the lane's largest entries.
+template <typename T, bool ALIGNED, int NW>
+__device__ __forceinline__ void gather_top(const ScoreArgs& a, const tiles::View& view, int n_groups, int first_tile, int tile_step, float even, float odd, const float* group_max,
+                                           TopSmem<NW>& sm, uint32_t blocks) {
+    using P = tiles::Packed16<T>;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    if (NW > 1) sm.bucket[warp][lane] = even, sm.bucket[warp][lane + 32] = odd;
+    __syncthreads();
     if (warp == 0) {
         for (int i = 1; i < NW; ++i) even = fmaxf(even, sm.bucket[i][lane]), odd = fmaxf(odd, sm.bucket[i][lane + 32]);
-        const float b = bound_of_kth(even, odd, K);
-        if ((uint32_t)lane < blocks) tiles::store_at(&sm.bound[rank], (uint32_t)lane, b);
+        const float b = bound_of_kth(even, odd, a.K);
+        if (lane == 0) {
+            sm.bound = b;
+            if (blocks > 1) tiles::store_at(&sm.bounds[first_tile], 0, b);
+        }
     }
-}
-
-// The entries of the block's tiles that reach the row's bound, in the first block's list.
-template <typename T, bool ALIGNED, int NW>
-__device__ __forceinline__ void gather_top(const ScoreArgs& a, const tiles::View& view, int n_groups, int first_tile, int tile_step, const float* group_max, TopSmem<NW>& sm,
-                                           uint32_t blocks) {
-    using P = tiles::Packed16<T>;
-    const int tid = threadIdx.x;
-    float bound = sm.bound[0];
-    for (uint32_t i = 1; i < blocks; ++i) bound = fmaxf(bound, sm.bound[i]);
+    __syncthreads();
+    const float bound = sm.bound;
     for (int i = tid; i < n_groups; i += NW * 32)
         if (group_max[i] >= bound && group_max[i] > kNegInf) {
             const int at = atomicAdd(&sm.groups, 1);
@@ -220,24 +222,42 @@ __device__ __forceinline__ void gather_top(const ScoreArgs& a, const tiles::View
     const int groups = sm.groups;
     if (groups > kList) {
         if (tid == 0) tiles::store_at(&sm.overflow, 0, 1);
-    } else {
-        for (int i = tid; i < groups * kWords; i += NW * 32) {
-            // group i: lane i & 31 of the block's (i >> 5)-th tile
-            const int g = sm.group[i / kWords], t = first_tile + (g >> 5) * tile_step, x0 = ((t * kWords + i % kWords) * 32 + (g & 31)) * P::kEntries;
-            const uint4 w = tiles::load_word<T, ALIGNED>(view, x0, a.V);
-#pragma unroll
-            for (int j = 0; j < P::kEntries; ++j) {
-                const float v = P::get(w, j);
-                if (v >= bound && v > kNegInf && v < __builtin_huge_valf()) {
-                    const int at = tiles::add_at(&sm.all_count, 0, 1);
-                    if (at < kList) {
-                        tiles::store_at(&sm.all_value[at], 0, v);
-                        tiles::store_at(&sm.all_token[at], 0, x0 + j);
-                    }
-                }
-            }
-        }
+        return;
     }
+    for (int i = tid; i < groups * kWords; i += NW * 32) {
+        // group i: lane i & 31 of the block's (i >> 5)-th tile
+        const int g = sm.group[i / kWords], t = first_tile + (g >> 5) * tile_step, x0 = ((t * kWords + i % kWords) * 32 + (g & 31)) * P::kEntries;
+        const uint4 w = tiles::load_word<T, ALIGNED>(view, x0, a.V);
+        uint32_t reach = 0;
+#pragma unroll
+        for (int j = 0; j < P::kEntries; ++j) {
+            const float v = P::get(w, j);
+            if (v >= bound && v > kNegInf && v < __builtin_huge_valf()) reach |= 1u << j;
+        }
+        if (!reach) continue;
+        int at = blocks > 1 ? tiles::add_at(&sm.count, 0, __popc(reach)) : atomicAdd(&sm.count, __popc(reach));
+#pragma unroll
+        for (int j = 0; j < P::kEntries; ++j)
+            if (reach >> j & 1) {
+                if (at < kList) {
+                    if (blocks > 1) tiles::store_at(&sm.key[at], 0, key_of(P::get(w, j), x0 + j));
+                    else sm.key[at] = key_of(P::get(w, j), x0 + j);
+                }
+                ++at;
+            }
+    }
+}
+
+// In the first block: what is left of the list at the largest of the blocks' bounds, in order of no kind, in place of the groups' list.
+template <int NW>
+__device__ __forceinline__ int keep_top(TopSmem<NW>& sm, uint32_t blocks) {
+    if (blocks == 1) return sm.count;
+    float bound = sm.bounds[0];
+    for (uint32_t i = 1; i < blocks; ++i) bound = fmaxf(bound, sm.bounds[i]);
+    for (int i = threadIdx.x; i < sm.count; i += NW * 32)
+        if (value_of(sm.key[i]) >= bound) sm.group[atomicAdd(&sm.kept, 1)] = i;
+    __syncthreads();
+    return sm.kept;
 }
 
 // Row r of sequence b, and the token that the accepted path has there; false: the slot is empty.
@@ -271,7 +291,7 @@ __global__ void __launch_bounds__(NW * 32, 32 / NW) score_rows_kernel(const __gr
     const uint32_t rank = tiles::cluster_rank(), blocks = tiles::cluster_blocks();
     if (tid == 0) {
         status_of_row = 0;
-        if constexpr (TOP) top_store.groups = top_store.all_count = top_store.overflow = 0;
+        if constexpr (TOP) top_store.groups = top_store.count = top_store.kept = top_store.overflow = 0;
     }
     if (blocks > 1) tiles::cluster_arrive();       // (the row's other blocks have started, and their words above are set, behind the wait below)
     grid_wait();
@@ -282,13 +302,6 @@ __global__ void __launch_bounds__(NW * 32, 32 / NW) score_rows_kernel(const __gr
     int32_t path_token;
     const char* row;
     const bool there = slot_of(a, slot, b, r, row, (int)sizeof(T), path_token, status);
-    int32_t token = -1;
-    float value = kNegInf;
-    if (rank == 0 && tid < a.T) {
-        token = a.accepted_len ? path_token : a.token ? a.token[slot * a.T + tid] : -1;
-        if (token >= a.V) token = -1, status |= RSD_ST_BAD_INDEX;
-        if (there && token >= 0) value = entry<T>(row, token);
-    }
     const tiles::View view = tiles::view_of<T>(row, a.V);
     const int all_tiles = tiles::tiles_of<T>(a.V, kWords), n_tiles = there ? all_tiles : 0;
     const Sums sums(dynamic, all_tiles);
@@ -297,6 +310,8 @@ __global__ void __launch_bounds__(NW * 32, 32 / NW) score_rows_kernel(const __gr
     const int step = NW * (int)blocks;
     int t = warp * (int)blocks + (int)rank;
     load_half<T, ALIGNED>(w, view, t, 0, lane, there ? a.V : 0), load_half<T, ALIGNED>(w, view, t, kWords / 2, lane, there ? a.V : 0);
+    int32_t token = path_token;
+    if (rank == 0 && tid < a.T && !a.accepted_len) token = a.token[slot * a.T + tid];
     if (blocks > 1) tiles::cluster_wait();
     else __syncthreads();
     float even = kNegInf, odd = kNegInf;
@@ -311,27 +326,31 @@ __global__ void __launch_bounds__(NW * 32, 32 / NW) score_rows_kernel(const __gr
             else even = fmaxf(even, lane_max);
         }
     }
+    float value = kNegInf;
+    if (rank == 0 && tid < a.T) {
+        if (token >= a.V) token = -1, status |= RSD_ST_BAD_INDEX;
+        if (there && token >= 0) value = entry<T>(row, token);
+    }
     if (bad) status |= RSD_ST_NAN_INPUT;
     if (status) tiles::or_at(&status_of_row, 0, status);
-    if constexpr (TOP) block_bound<NW>(top_store, even, odd, a.K, rank, blocks);
+    if constexpr (TOP)
+        gather_top<T, ALIGNED, NW>(a, view, there ? (n_tiles - (int)rank + (int)blocks - 1) / (int)blocks * 32 : 0, (int)rank, (int)blocks, even, odd, group_max, top_store, blocks);
     tiles::row_barrier(blocks);
-    if (rank == 0 && warp == 0) {
-        const RowTotals t = join<true>(sums, n_tiles, a.k, lane);
-        if (lane == 0) total_of_row = t;
-    }
-    if constexpr (TOP) {
-        gather_top<T, ALIGNED, NW>(a, view, there ? (n_tiles - (int)rank + (int)blocks - 1) / (int)blocks * 32 : 0, (int)rank, (int)blocks, group_max, top_store, blocks);
-        tiles::row_barrier(blocks);
-    }
     if (rank != 0) {
         grid_started();
         return;
     }
-    if constexpr (TOP) {
-        if (top_store.overflow || top_store.all_count > kList) top_one_by_one<T, NW>(row, a.V, a.K, top_store);
-    } else {
-        __syncthreads();
+    if (warp == 0) {
+        const RowTotals t = join<true>(sums, n_tiles, a.k, lane);
+        if (lane == 0) total_of_row = t;
     }
+    int kept = 0;
+    if constexpr (TOP) {
+        const bool beyond = top_store.overflow || top_store.count > kList;
+        if (beyond) top_one_by_one<T, NW>(row, a.V, a.K, top_store);
+        kept = keep_top<NW>(top_store, beyond ? 1 : blocks);
+    }
+    __syncthreads();
     const RowTotals total = total_of_row;
     const bool none = !there || total.m == kNegInf;
     const float lnz = none ? 0.0f : logf(total.s);
@@ -343,16 +362,17 @@ __global__ void __launch_bounds__(NW * 32, 32 / NW) score_rows_kernel(const __gr
     bool few = false;
     if constexpr (TOP) {
         const TopSmem<NW>& top = top_store;
-        const int n = there ? top.all_count : 0;
+        const bool in_place = blocks == 1 || top.overflow || top.kept == 0;
+        const int n = there ? kept : 0;
         few = there && n < a.K;
         for (int i = tid; i < n; i += NW * 32) {
-            const float v = top.all_value[i];
-            const int x = top.all_token[i];
+            const unsigned long long key = top.key[in_place ? i : top.group[i]];
             int place = 0;
-            for (int j = 0; j < n; ++j) place += top.all_value[j] > v || (top.all_value[j] == v && top.all_token[j] < x);
+#pragma unroll 4
+            for (int j = 0; j < n; ++j) place += top.key[in_place ? j : top.group[j]] > key;
             if (place < a.K) {
-                a.out_top_token[slot * a.K + place] = x;
-                a.out_top_logprob[slot * a.K + place] = logprob(v);
+                a.out_top_token[slot * a.K + place] = token_of(key);
+                a.out_top_logprob[slot * a.K + place] = logprob(value_of(key));
             }
         }
         for (int i = n + tid; i < a.K; i += NW * 32) a.out_top_token[slot * a.K + i] = -1, a.out_top_logprob[slot * a.K + i] = kNegInf;

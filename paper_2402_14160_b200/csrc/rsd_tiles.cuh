@@ -358,6 +358,9 @@ __device__ __forceinline__ uint32_t remote(const void* p, uint32_t rank) {   // 
 }
 __device__ __forceinline__ void store_at(float* p, uint32_t rank, float v) { asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(remote(p, rank)), "f"(v) : "memory"); }
 __device__ __forceinline__ void store_at(int* p, uint32_t rank, int v) { asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(remote(p, rank)), "r"(v) : "memory"); }
+__device__ __forceinline__ void store_at(unsigned long long* p, uint32_t rank, unsigned long long v) {
+    asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(remote(p, rank)), "l"(v) : "memory");
+}
 __device__ __forceinline__ void or_at(int* p, uint32_t rank, int v) { asm volatile("red.shared::cluster.or.b32 [%0], %1;" ::"r"(remote(p, rank)), "r"(v) : "memory"); }
 __device__ __forceinline__ void max_at(uint32_t* p, uint32_t rank, uint32_t v) { asm volatile("red.shared::cluster.max.u32 [%0], %1;" ::"r"(remote(p, rank)), "r"(v) : "memory"); }
 __device__ __forceinline__ int add_at(int* p, uint32_t rank, int v) {
