@@ -88,9 +88,10 @@ __device__ __noinline__ CarefulSums add_tile_careful(Words p, Words q, float mp,
 }
 
 // masked: the row's last tile had entries without mass, so that this one is looked through for them at once.
-template <typename T, bool BOTH>   // BOTH: the sums of weight times difference too
+// next() reads the warp's next tile into the words' places, ahead of the sums over the warp.
+template <typename T, bool BOTH, typename F>   // BOTH: the sums of weight times difference too
 __device__ __forceinline__ void tile_sums(uint4 (&p)[kWords], uint4 (&q)[kWords], float kp, float kq, int t, int lane, uint32_t blocks, Sums* sums, float& alone_p, float& alone_q,
-                                          bool& bad, bool& masked) {
+                                          bool& bad, bool& masked, F next) {
     using P = tiles::Packed16<T>;
     float mp = tiles::warp_max_nan(P::largest(p)), mq = tiles::warp_max_nan(P::largest(q));
     if (!(mp < __builtin_huge_valf()) || !(mq < __builtin_huge_valf())) {   // NaN or +inf: no entries
@@ -131,6 +132,7 @@ __device__ __forceinline__ void tile_sums(uint4 (&p)[kWords], uint4 (&q)[kWords]
         }
         halves();
     }
+    next();
     // Sums::sp, sq, dp, dq are in eight lanes each (without the last two in sixteen each); four lanes store them and two the largest entries, in every block.
     const float sum = BOTH ? tiles::warp_sum_four(sp, sq, dp, dq, lane) : tiles::warp_sum_two(sp, sq, lane);
     const int member = (lane & 4) ? 4 + (lane >> 4) : BOTH ? lane >> 3 : lane >> 4;
@@ -198,16 +200,19 @@ __device__ __forceinline__ bool read_rows(const DivergenceArgs& a, const Pair& w
     if (w.blocks > 1) tiles::cluster_arrive();     // (the pair's other blocks have started, and their words above are set, behind the wait below)
     else __syncthreads();
     grid_wait();
+    uint4 p[kWords], q[kWords];
+    auto load = [&](int t) {
+        if (t >= w.n_tiles) return;
+        tiles::load_tile<T, ALIGNED, kWords>(p, w.draft, t, lane, a.V);
+        tiles::load_tile<T, ALIGNED, kWords>(q, w.target, t, lane, a.V);
+    };
+    load(w.first);
     if (w.blocks > 1) tiles::cluster_wait();
     float alone_p = kNegInf, alone_q = kNegInf;
     bool bad = false, masked = false;
 #pragma unroll 1
-    for (int t = w.first; t < w.n_tiles; t += w.step) {
-        uint4 p[kWords], q[kWords];
-        tiles::load_tile<T, ALIGNED, kWords>(p, w.draft, t, lane, a.V);
-        tiles::load_tile<T, ALIGNED, kWords>(q, w.target, t, lane, a.V);
-        tile_sums<T, BOTH>(p, q, a.k_draft, a.k_target, t, lane, w.blocks, w.sums, alone_p, alone_q, bad, masked);
-    }
+    for (int t = w.first; t < w.n_tiles; t += w.step)
+        tile_sums<T, BOTH>(p, q, a.k_draft, a.k_target, t, lane, w.blocks, w.sums, alone_p, alone_q, bad, masked, [&] { load(t + w.step); });
     if (bad || alone_p > kNegInf || alone_q > kNegInf)
         for (uint32_t i = 0; i < w.blocks; ++i) {
             if (bad) tiles::or_at(&sm.status, i, RSD_ST_NAN_INPUT);
@@ -287,11 +292,15 @@ __global__ void __launch_bounds__(NW * 32, 32 / NW) divergence_kernel(const __gr
         const unsigned long long shift = tiles::both(q.off - p.off);
         auto sweep = [&](auto plain) {
             constexpr bool PLAIN = decltype(plain)::value;
-#pragma unroll 1
-            for (int t = w.first; t < w.n_tiles; t += w.step) {
-                uint4 pw[kWords], qw[kWords];
+            uint4 pw[kWords], qw[kWords];
+            auto load = [&](int t) {
+                if (t >= w.n_tiles) return;
                 tiles::load_tile<T, ALIGNED, kWords>(pw, w.draft, t, lane, a.V);
                 tiles::load_tile<T, ALIGNED, kWords>(qw, w.target, t, lane, a.V);
+            };
+            load(w.first);
+#pragma unroll 1
+            for (int t = w.first; t < w.n_tiles; t += w.step) {
                 if (bad) {
                     bool ignored = false;
 #pragma unroll
@@ -307,6 +316,7 @@ __global__ void __launch_bounds__(NW * 32, 32 / NW) divergence_kernel(const __gr
                         split_f32x2(add_f32x2(q.of<PLAIN>(P::pair(qw[i], j)), shift), u, v);
                         s = add_f32x2(s, f32x2(ex2_approx(fminf(x, u)), ex2_approx(fminf(y, v))));
                     }
+                load(t + w.step);
                 float x, y;
                 split_f32x2(s, x, y);
                 const float sum = tiles::warp_sum_two(x + y, 0.0f, lane);
