@@ -228,6 +228,9 @@ __device__ __forceinline__ bool read_rows(const DivergenceArgs& a, const Pair& w
     return sm.status != 0;
 }
 
+// The warp's last tile of n (negative: it has none).  Second sweeps go from there to the first one: what was read last is in L2 even where the pairs under way do not all fit.
+__device__ __forceinline__ int last_tile(const Pair& w, int n) { return w.first < n ? w.first + (n - 1 - w.first) / w.step * w.step : -1; }
+
 struct Result {
     bool empty, kl_infinite, reverse_infinite;
     float log2_sp, log2_sq;
@@ -294,13 +297,14 @@ __global__ void __launch_bounds__(NW * 32, 32 / NW) divergence_kernel(const __gr
             constexpr bool PLAIN = decltype(plain)::value;
             uint4 pw[kWords], qw[kWords];
             auto load = [&](int t) {
-                if (t >= w.n_tiles) return;
+                if (t < 0) return;
                 tiles::load_tile<T, ALIGNED, kWords>(pw, w.draft, t, lane, a.V);
                 tiles::load_tile<T, ALIGNED, kWords>(qw, w.target, t, lane, a.V);
             };
-            load(w.first);
+            const int last = last_tile(w, w.n_tiles);
+            load(last);
 #pragma unroll 1
-            for (int t = w.first; t < w.n_tiles; t += w.step) {
+            for (int t = last; t >= 0; t -= w.step) {
                 if (bad) {
                     bool ignored = false;
 #pragma unroll
@@ -316,7 +320,7 @@ __global__ void __launch_bounds__(NW * 32, 32 / NW) divergence_kernel(const __gr
                         split_f32x2(add_f32x2(q.of<PLAIN>(P::pair(qw[i], j)), shift), u, v);
                         s = add_f32x2(s, f32x2(ex2_approx(fminf(x, u)), ex2_approx(fminf(y, v))));
                     }
-                load(t + w.step);
+                load(t - w.step);
                 float x, y;
                 split_f32x2(s, x, y);
                 const float sum = tiles::warp_sum_two(x + y, 0.0f, lane);
@@ -376,9 +380,9 @@ __global__ void __launch_bounds__(NW * 32, 24 / NW) divergence_grad_kernel(const
         });
     };
     auto write = [&](auto plain) {
-        const int last = tiles::tiles_of<T>(head + a.V, kWords);    // tiles of the gradient: `head` entries ahead of the rows'
+        // tiles of the gradient: `head` entries ahead of the rows'
 #pragma unroll 1
-        for (int t = w.first; t < last; t += w.step) {
+        for (int t = last_tile(w, tiles::tiles_of<T>(head + a.V, kWords)); t >= 0; t -= w.step) {
             const int x = t * kTile - head + lane * E;
             char* const to = grad + (int64_t)x * (int)sizeof(T);
             const bool whole = t * kTile >= head && (t + 1) * kTile - head <= a.V;
