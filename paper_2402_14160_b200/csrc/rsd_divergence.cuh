@@ -193,7 +193,7 @@ __device__ __forceinline__ Pair pair_of(const DivergenceArgs& a, unsigned char* 
 }
 
 // Both rows, read into the tiles' sums; everything else of a pair follows from what this leaves in every block's shared memory.  True: there were NaN or +inf.
-template <typename T, bool ALIGNED, bool BOTH, int NW>
+template <typename T, bool ALIGNED, bool BOTH, int NW, int USE>
 __device__ __forceinline__ bool read_rows(const DivergenceArgs& a, const Pair& w, Smem& sm) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     if (threadIdx.x == 0) sm.status = 0, sm.alone_p = sm.alone_q = 0;
@@ -203,8 +203,8 @@ __device__ __forceinline__ bool read_rows(const DivergenceArgs& a, const Pair& w
     uint4 p[kWords], q[kWords];
     auto load = [&](int t) {
         if (t >= w.n_tiles) return;
-        tiles::load_tile<T, ALIGNED, kWords>(p, w.draft, t, lane, a.V);
-        tiles::load_tile<T, ALIGNED, kWords>(q, w.target, t, lane, a.V);
+        tiles::load_tile<T, ALIGNED, kWords, USE>(p, w.draft, t, lane, a.V);
+        tiles::load_tile<T, ALIGNED, kWords, USE>(q, w.target, t, lane, a.V);
     };
     load(w.first);
     if (w.blocks > 1) tiles::cluster_wait();
@@ -274,14 +274,14 @@ __device__ __forceinline__ LogProb log_prob(float m, float k, float log2s, bool 
     return l;
 }
 
-template <typename T, bool ALIGNED, int NW>
+template <typename T, bool ALIGNED, bool OVERLAP, int NW>
 __global__ void __launch_bounds__(NW * 32, 32 / NW) divergence_kernel(const __grid_constant__ DivergenceArgs a) {
     using P = tiles::Packed16<T>;
     extern __shared__ __align__(16) unsigned char dynamic_bytes[];   // all tiles' sums
     __shared__ Smem sm;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const Pair w = pair_of<T, NW>(a, dynamic_bytes);
-    const bool bad = read_rows<T, ALIGNED, true, NW>(a, w, sm);
+    const bool bad = read_rows<T, ALIGNED, true, NW, OVERLAP ? tiles::kReadFirst : tiles::kReadOnce>(a, w, sm);
     const Result res = result_of(a, sm);
     if (w.rank == 0 && tid == 0) {
         const Totals& t = sm.total;
@@ -290,7 +290,7 @@ __global__ void __launch_bounds__(NW * 32, 32 / NW) divergence_kernel(const __gr
         if (a.out_reverse) a.out_reverse[w.slot] = res.empty ? 0.0f : res.reverse_infinite ? inf : divergence_of(t.dp, t.sp, t.sq);
         a.status[w.slot] = status_of(res, bad);
     }
-    if (a.out_overlap) {
+    if constexpr (OVERLAP) {
         const LogProb p = log_prob(sm.total.mp, a.k_draft, res.log2_sp, res.empty), q = log_prob(sm.total.mq, a.k_target, res.log2_sq, res.empty);
         const unsigned long long shift = tiles::both(q.off - p.off);
         auto sweep = [&](auto plain) {
@@ -298,8 +298,8 @@ __global__ void __launch_bounds__(NW * 32, 32 / NW) divergence_kernel(const __gr
             uint4 pw[kWords], qw[kWords];
             auto load = [&](int t) {
                 if (t < 0) return;
-                tiles::load_tile<T, ALIGNED, kWords>(pw, w.draft, t, lane, a.V);
-                tiles::load_tile<T, ALIGNED, kWords>(qw, w.target, t, lane, a.V);
+                tiles::load_tile<T, ALIGNED, kWords, tiles::kReadLast>(pw, w.draft, t, lane, a.V);
+                tiles::load_tile<T, ALIGNED, kWords, tiles::kReadLast>(qw, w.target, t, lane, a.V);
             };
             const int last = last_tile(w, w.n_tiles);
             load(last);
@@ -352,7 +352,7 @@ __global__ void __launch_bounds__(NW * 32, 24 / NW) divergence_grad_kernel(const
     __shared__ Smem sm;
     const int tid = threadIdx.x, lane = tid & 31;
     const Pair w = pair_of<T, NW>(a, dynamic_bytes);
-    const bool bad = read_rows<T, ALIGNED, REVERSE, NW>(a, w, sm);
+    const bool bad = read_rows<T, ALIGNED, REVERSE, NW, tiles::kReadFirst>(a, w, sm);
     const float g = a.g_kl ? a.g_kl[w.slot] : 0.0f, h = REVERSE ? a.g_reverse[w.slot] : 0.0f;
     const Result res = result_of(a, sm);
     const float gt = res.empty ? 0.0f : g * a.inv_draft_temp, ht = res.empty || (REVERSE && res.reverse_infinite) ? 0.0f : h * a.inv_draft_temp;
@@ -387,8 +387,8 @@ __global__ void __launch_bounds__(NW * 32, 24 / NW) divergence_grad_kernel(const
             char* const to = grad + (int64_t)x * (int)sizeof(T);
             const bool whole = t * kTile >= head && (t + 1) * kTile - head <= a.V;
             uint4 pw[kWords], qw[kWords];
-            tiles::load_words<T, ALIGNED, kWords>(pw, w.draft, x, whole, a.V);
-            tiles::load_words<T, ALIGNED, kWords>(qw, w.target, x, whole, a.V);
+            tiles::load_words<T, ALIGNED, kWords, tiles::kReadLast>(pw, w.draft, x, whole, a.V);
+            tiles::load_words<T, ALIGNED, kWords, tiles::kReadLast>(qw, w.target, x, whole, a.V);
             if (bad) {
                 bool ignored = false;
 #pragma unroll

@@ -100,26 +100,32 @@ inline int divergence_warps(unsigned slots, int n_tiles, bool one_sweep) {
     if (n_tiles <= 8 || (n_tiles <= 16 && slots > 2u * sms) || (one_sweep && slots > 4u * sms)) return 4;
     return 8;
 }
-template <typename T, bool ALIGNED, int NW>
+template <typename T, bool ALIGNED, bool OVERLAP, int NW>
 void launch_divergence_as(unsigned slots, int blocks, const DivergenceArgs& a, cudaStream_t s) {
-    launch_rows(divergence::divergence_kernel<T, ALIGNED, NW>, slots, blocks, NW * 32, (size_t)tiles::tiles_of<T>(a.V, divergence::kWords) * sizeof(divergence::Sums), s, a);
+    launch_rows(divergence::divergence_kernel<T, ALIGNED, OVERLAP, NW>, slots, blocks, NW * 32, (size_t)tiles::tiles_of<T>(a.V, divergence::kWords) * sizeof(divergence::Sums), s, a);
 }
-template <typename T, bool ALIGNED>
+template <typename T, bool ALIGNED, bool OVERLAP>
 void launch_divergence_warps(unsigned slots, const DivergenceArgs& a, cudaStream_t s) {
-    const int n_tiles = tiles::tiles_of<T>(a.V, divergence::kWords), blocks = row_blocks(slots, n_tiles, 8), warps = blocks > 1 ? 8 : divergence_warps(slots, n_tiles, !a.out_overlap);
-    if (warps == 8) launch_divergence_as<T, ALIGNED, 8>(slots, blocks, a, s);
-    else if (warps == 4) launch_divergence_as<T, ALIGNED, 4>(slots, 1, a, s);
-    else launch_divergence_as<T, ALIGNED, 2>(slots, 1, a, s);
+    const int n_tiles = tiles::tiles_of<T>(a.V, divergence::kWords), blocks = row_blocks(slots, n_tiles, 8), warps = blocks > 1 ? 8 : divergence_warps(slots, n_tiles, !OVERLAP);
+    if (warps == 8) launch_divergence_as<T, ALIGNED, OVERLAP, 8>(slots, blocks, a, s);
+    else if (warps == 4) launch_divergence_as<T, ALIGNED, OVERLAP, 4>(slots, 1, a, s);
+    else launch_divergence_as<T, ALIGNED, OVERLAP, 2>(slots, 1, a, s);
 }
 template <typename T>
 void launch_divergence_of(bool aligned, unsigned slots, const DivergenceArgs& a, cudaStream_t s) {
-    if (aligned) launch_divergence_warps<T, true>(slots, a, s);
-    else launch_divergence_warps<T, false>(slots, a, s);
+    if (a.out_overlap) {
+        if (aligned) launch_divergence_warps<T, true, true>(slots, a, s);
+        else launch_divergence_warps<T, false, true>(slots, a, s);
+    } else {
+        if (aligned) launch_divergence_warps<T, true, false>(slots, a, s);
+        else launch_divergence_warps<T, false, false>(slots, a, s);
+    }
 }
 
-// Gradients of divergences read their rows twice, the second time from L2, which holds about 64 MB of them beside the gradient's words: long rows are shared by two or four blocks, so that fewer
-// are under way at a time (us, 1 / 2 / 4 / 8 blocks: 1000 pairs of 60,000 bf16 104 / 93 / 109 / 149, of 60,000 fp32 203 / 194 / 181 / 208, of 128,000 bf16 212 / 205 / 195 / 240).
-constexpr int64_t kReadAgainBytes = 64 << 20;
+// Gradients of divergences read their rows twice, the second time from L2, which does not hold the pairs under way beside the gradient's words where they are long: those are shared by two or four
+// blocks, so that fewer are under way at a time (us, 1 / 2 / 4 / 8 blocks: 1000 pairs of 32,000 fp32 91 / 89 / 108 / 150, of 60,000 fp32 180 / 159 / 159 / 201, of 128,000 bf16
+// 193 / 179 / 184 / 229, of 128,000 fp32 390 / 355 / 328 / 337; 5000 of 60,000 bf16 387 / 405 / 506 / 713).
+constexpr int64_t kReadAgainBytes = 120 * 1000 * 1000;
 template <typename T, bool ALIGNED, bool REVERSE, int NW>
 void launch_divergence_grad_as(unsigned slots, int blocks, const DivergenceArgs& a, cudaStream_t s) {
     launch_rows(divergence::divergence_grad_kernel<T, ALIGNED, REVERSE, NW>, slots, blocks, NW * 32, (size_t)tiles::tiles_of<T>(a.V, divergence::kWords) * sizeof(divergence::Sums), s, a);
