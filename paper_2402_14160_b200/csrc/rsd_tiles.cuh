@@ -207,7 +207,7 @@ template <typename T>
 __host__ __device__ constexpr int tiles_of(int V, int KW) { return (V + tile_entries<T>(KW) - 1) / tile_entries<T>(KW); }
 
 // What L2 is told about a row's words: nothing, that they are read again soon, or that they are read for the last time.  (Two sweeps over more rows than fit beside what is written:
-// gradients of 7000 pairs of 32,000 bf16 319 -> 278 us, divergences of as many fp32 pairs 457 -> 375; rows read once are 4 % slower when they are to be kept, and so are shifted rows, whose words come through L1.)
+// gradients of 7000 pairs of 32,000 bf16 319 -> 278 us, divergences of as many fp32 pairs 457 -> 375; rows read once are 4 % slower when they are to be kept, and so are rows off the boundaries.)
 enum { kReadOnce = 0, kReadFirst = 1, kReadLast = 2 };
 template <int USE>
 __device__ __forceinline__ uint64_t l2_policy() {
@@ -254,7 +254,7 @@ __device__ __forceinline__ void load_words(uint4 (&w)[KW], const View& v, int x0
         const char* p = v.base + (at & ~15);
         if (ALIGNED || shift == 0) {
 #pragma unroll
-            for (int k = 0; k < KW; ++k) w[k] = ld_use<USE>(p + k * 512);
+            for (int k = 0; k < KW; ++k) w[k] = ld_use<ALIGNED ? USE : kReadOnce>(p + k * 512);
         } else {                                   // (the word's last entry lies in the second granule)
             with_shift(shift, [&](auto q) {
 #pragma unroll
