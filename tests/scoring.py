@@ -49,6 +49,8 @@ def top(rows, K):
 
 def close(got, want, tol, what):
     got, want = got.double(), want.double()
+    beyond = want.abs() > torch.finfo(torch.float32).max        # (values beyond fp32's range are infinite there)
+    want = torch.where(beyond, torch.sign(want) * float("inf"), want)
     tol = torch.as_tensor(tol, dtype=torch.float64, device=want.device).expand_as(want)
     fine = torch.isfinite(want)
     assert torch.equal(torch.isfinite(got), fine), what + ": not finite at other places"
@@ -100,13 +102,15 @@ def score_gradient(rows, token, g, h, T):
         h = h.double()[..., None]
         grad = grad - h * p * (lp0 + H)
         size = size + h.abs() * p * (lp0.abs() + H + 1)
-    spike = torch.zeros_like(grad)
+    spike, spikes = torch.zeros_like(grad), torch.zeros_like(grad)
     for t in range(tok.shape[-1]):
-        spike.scatter_add_(-1, torch.where(there, tok, 0)[..., t:t + 1].long(), g[..., t:t + 1])
+        at = torch.where(there, tok, 0)[..., t:t + 1].long()
+        spike.scatter_add_(-1, at, g[..., t:t + 1])
+        spikes.scatter_add_(-1, at, g[..., t:t + 1].abs())
     empty = lp.amax(-1, keepdim=True) == NEG
     grad = torch.where(empty, 0.0, (grad + spike) / T)
-    # p is off by SUM and by the rounding of its exponent, the factors by a few roundings
-    bound = (size * (2 * SUM + 4 * EPS * lp0.abs()) + 8 * EPS * (spike.abs() + size) + 64 * EPS * size) / T
+    # p is off by SUM and by the rounding of its exponent, the factors by a few roundings, a sum of T weights by as many of the sum of their sizes
+    bound = (size * (2 * SUM + 4 * EPS * lp0.abs()) + (8 + tok.shape[-1]) * EPS * (spikes + size) + 64 * EPS * size) / T
     return grad, bound + flushed(p, size, T)
 
 
