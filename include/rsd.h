@@ -319,7 +319,7 @@ int rsd_resample_residual(const rsd_rows* draft_row, const rsd_rows* target_row,
  *   out_top_token, out_top_logprob   [B][R][K] int32 / fp32, K <= RSD_MAX_K (K = 0: NULL): the K largest entries in decreasing order,
  *                equal values to the smaller token, and their ln p; -1 and -inf beyond the row's entries (RSD_ST_FEWER_THAN_K)
  *   status       [B][R], of each slot
- * Outputs may not overlap the inputs or each other.
+ * A log-probability beyond fp32's range is -inf.  Outputs may not overlap the inputs or each other.
  */
 int rsd_token_logprobs(const rsd_rows* rows, int B, int R, int V, int num_rows, const int32_t* row_index, const int32_t* token, int T,
                        int K, float* out_logprob, float* out_entropy, int32_t* out_top_token, float* out_top_logprob,

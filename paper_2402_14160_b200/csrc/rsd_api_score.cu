@@ -114,6 +114,7 @@ int rsd_token_logprobs_backward(const rsd_rows* rows, int B, int R, int V, const
     if (int e = check_batch(B, R)) return e;
     if (T < 1 || T > RSD_MAX_K) return fail(RSD_ERR_UNSUPPORTED, "T = %d outside [1, %d]", T, (int)RSD_MAX_K);
     if (!token || !grad_logprob || !grad_rows || !status) return fail(RSD_ERR_INVALID_ARG, "null argument");
+    if (grad_rows == rows->data) return fail(RSD_ERR_INVALID_ARG, "grad_rows may not overlap the rows");
     if (B == 0) return RSD_OK;
     cudaStream_t s = (cudaStream_t)stream;
     rsd::ScoreArgs a = score_args(rows, R, V, T, 0);
@@ -146,6 +147,7 @@ int rsd_row_divergence_backward(const rsd_rows* draft, const rsd_rows* target, i
     g_err[0] = 0;
     if (int e = check_pair(draft, target, B, R, V)) return e;
     if (!status || !grad_draft || (!grad_kl && !grad_reverse_kl)) return fail(RSD_ERR_INVALID_ARG, "null argument");
+    if (grad_draft == draft->data || grad_draft == target->data) return fail(RSD_ERR_INVALID_ARG, "grad_draft may not overlap the rows");
     if (B == 0) return RSD_OK;
     cudaStream_t s = (cudaStream_t)stream;
     rsd::DivergenceArgs a = divergence_args(draft, target, R, V);

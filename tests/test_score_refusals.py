@@ -48,7 +48,7 @@ def test_emitted_logprobs(change, code, text):
 
 @pytest.mark.parametrize("change, code, text", [
     (dict(T=0), 2, b"T = 0"), (dict(T=33), 2, b"T = 33"), (dict(token=None), 1, b"null"), (dict(g=None), 1, b"null"), (dict(grad=None), 1, b"null"), (dict(status=None), 1, b"null"),
-    (dict(R=0), 1, b"R = 0"), (dict(V=0), 2, b"V = 0")])
+    (dict(R=0), 1, b"R = 0"), (dict(V=0), 2, b"V = 0"), (dict(), 1, b"overlap")])
 def test_token_logprobs_backward(change, code, text):
     a = dict(rows=_rows(), B=1, R=2, V=64, token=PTR, T=1, g=PTR, h=None, grad=PTR, status=PTR, stream=None)
     a.update(change)
@@ -66,7 +66,8 @@ def test_row_divergence(change, code, text):
 
 
 @pytest.mark.parametrize("change, code, text", [
-    (dict(g=None, h=None), 1, b"null"), (dict(grad=None), 1, b"null"), (dict(status=None), 1, b"null"), (dict(target=_rows(api.RSD_BF16)), 2, b"same dtype")])
+    (dict(g=None, h=None), 1, b"null"), (dict(grad=None), 1, b"null"), (dict(status=None), 1, b"null"), (dict(target=_rows(api.RSD_BF16)), 2, b"same dtype"),
+    (dict(), 1, b"overlap"), (dict(draft=_rows(data=2 * PTR)), 1, b"overlap")])
 def test_row_divergence_backward(change, code, text):
     a = dict(draft=_rows(), target=_rows(), B=1, R=2, V=64, g=PTR, h=None, grad=PTR, status=PTR, stream=None)
     a.update(change)
