@@ -370,13 +370,13 @@ __global__ void __launch_bounds__(NW * 32, 24 / NW) divergence_grad_kernel(const
     // gt (p - q) + p ht (ln 2 (log2 p - log2 q) - KL(p||q)); rows that are equal give 0
     const float reverse = REVERSE && ht != 0.0f ? 0.69314718f * (__fdividef(sm.total.dp, sm.total.sp) + res.log2_sq - res.log2_sp) : 0.0f;
     const float c1f = ht * 0.69314718f, c0f = fmaf(c1f, lp.off - lq.off, -ht * reverse);
-    const unsigned long long c0 = tiles::both(c0f * scale_p), c1 = tiles::both(c1f * scale_p), cg = tiles::both(gt * scale_p), minus_ratio = tiles::both(-__fdividef(scale_q, scale_p)),
+    const unsigned long long c0 = tiles::both(tiles::held_to(c0f * scale_p, 1e38f)), c1 = tiles::both(tiles::held_to(c1f * scale_p, tiles::kMostFactor)),
+                             cg = tiles::both(tiles::held_to(gt * scale_p, 1e38f)), minus_ratio = tiles::both(-__fdividef(scale_q, scale_p)),
                              minus_one = tiles::both(-1.0f);
     char* const grad = (char*)a.grad + w.slot * a.V * (int64_t)sizeof(T);
     const int head = ALIGNED ? 0 : (int)((uintptr_t)grad & 15u) / (int)sizeof(T);   // entries between the boundary and the gradient's first one
-    auto word = [&](uint4 pw, uint4 qw, auto plain) {
+    auto word = [&](const uint4& pw, const uint4& qw, auto plain) {
         constexpr bool PLAIN = decltype(plain)::value;
-        if (REVERSE && PLAIN) pw = P::raised(pw), qw = P::raised(qw);
         return P::make([&](int i) {
             float x, y, u, v;
             split_f32x2(lp.of<PLAIN>(P::pair(pw, i)), x, y);
@@ -384,7 +384,7 @@ __global__ void __launch_bounds__(NW * 32, 24 / NW) divergence_grad_kernel(const
             const unsigned long long wp = f32x2(ex2_approx(x), ex2_approx(y)), wq = f32x2(ex2_approx(u), ex2_approx(v));
             const unsigned long long apart = tiles::mul_f32x2(fma_f32x2(wq, minus_ratio, wp), cg);
             if (!REVERSE) return apart;
-            if (!PLAIN) x = fmaxf(x, tiles::kFarBelow), y = fmaxf(y, tiles::kFarBelow), u = fmaxf(u, tiles::kFarBelow), v = fmaxf(v, tiles::kFarBelow);
+            x = fmaxf(x, tiles::kNoWeight), y = fmaxf(y, tiles::kNoWeight), u = fmaxf(u, tiles::kNoWeight), v = fmaxf(v, tiles::kNoWeight);
             return fma_f32x2(wp, fma_f32x2(fma_f32x2(f32x2(u, v), minus_one, f32x2(x, y)), c1, c0), apart);
         });
     };

@@ -395,7 +395,8 @@ __global__ void __launch_bounds__(NW * 32, 32 / NW) score_rows_kernel(const __gr
 // A block has consecutive tiles of its row and keeps them in shared memory for the second sweep (read again from L2, the
 // gradient's own words pushed two thirds of the rows out to memory); words of the gradient are written on their own 16-byte boundaries.
 //
-// 8192 rows of 32,000 bf16 with an entropy term: 201 us = 5.2 TB/s read and written, 0.79 of the measured copy bandwidth (sustained, at the power limit, 218).  Three rows an SM are what
+// 8192 rows of 32,000 bf16 with an entropy term: 210 us = 5.0 TB/s read and written, 0.76 of the measured copy bandwidth (sustained, at the power limit, 228; 9 us of it
+// are the limits under which masked entries get 0 whatever the factors).  Three rows an SM are what
 // shared memory holds, 24 warps; two exponentials an entry keep the special-function unit 60 % busy, and the warps wait for each other at the two barriers (15 % of
 // the stalls) and for the unit's queue.  Slower: blocks that stay for several rows and ask for the next one early (224: without arithmetic 180 against 159), 4 warps a row (225).
 struct Slope {                     // gradient of an entry without a token: p (c0 + c1 log2 p),   log2 p = v k - c (plain rows) or (v - m) k - c
@@ -412,7 +413,7 @@ __device__ __forceinline__ Slope slope_of(const RowTotals& total, float G, float
     const float off = f.plain ? -(fmaf(total.m, k, -f.c) + log2s) : 0.0f, scale = ex2_approx(off);
     f.c1 = f.none ? 0.0f : -h * 0.69314718f * inv_temp;
     f.c0 = f.none ? 0.0f : fmaf(f.c1, off, -(G + h * H) * inv_temp) * scale;
-    f.c1 *= scale;
+    f.c0 = tiles::held_to(f.c0, 1e38f), f.c1 = tiles::held_to(f.c1 * scale, tiles::kMostFactor);
     return f;
 }
 
@@ -485,13 +486,12 @@ __global__ void __launch_bounds__(NW * 32, 24 / NW) score_grad_kernel(const __gr
         float x, y;
         const unsigned long long l = fma_f32x2(decltype(plain_row)::value ? v : add_f32x2(v, minus_m), kk, minus_c);
         split_f32x2(l, x, y);
-        if (ENTROPY && !decltype(plain_row)::value) x = fmaxf(x, tiles::kFarBelow), y = fmaxf(y, tiles::kFarBelow);
+        if (ENTROPY) x = fmaxf(x, tiles::kNoWeight), y = fmaxf(y, tiles::kNoWeight);
         const unsigned long long p = f32x2(ex2_approx(x), ex2_approx(y));
         return tiles::mul_f32x2(p, ENTROPY ? fma_f32x2(f32x2(x, y), c1, c0) : c0);
     };
     const int head = ALIGNED ? 0 : (int)((uintptr_t)grad & 15u) / (int)sizeof(T);   // entries between the boundary and the gradient's first one
-    auto word = [&](uint4 v, auto plain_row) {
-        if (ENTROPY && decltype(plain_row)::value) v = P::raised(v);
+    auto word = [&](const uint4& v, auto plain_row) {
         return P::make([&](int i) { return slope(P::pair(v, i), plain_row); });
     };
     auto write = [&](auto plain_row) {
@@ -534,8 +534,8 @@ __global__ void __launch_bounds__(NW * 32, 24 / NW) score_grad_kernel(const __gr
                     if (tokens[i] == mine) own += weights[i], first = first && i >= lane;
                 if (first) {
                     const int at = view.first + mine * (int)sizeof(T) - t0 * kWords * 512, tile = min(at / (kWords * 512), t1 - t0 - 1);
-                    float v = at >= 0 ? entry<T>(dynamic_bytes + at + tile * 16, 0) : entry<T>(view.base + view.first, mine), rest, ignored;
-                    if (decltype(plain_row)::value) v = fmaxf(v, tiles::kLow);
+                    const float v = at >= 0 ? entry<T>(dynamic_bytes + at + tile * 16, 0) : entry<T>(view.base + view.first, mine);
+                    float rest, ignored;
                     split_f32x2(slope(tiles::both(v), plain_row), rest, ignored);
                     P::store(grad, mine, f.none ? 0.0f : fmaf(own, f.inv_temp, rest));
                 }

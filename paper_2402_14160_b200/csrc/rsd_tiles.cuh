@@ -46,7 +46,8 @@ __device__ __forceinline__ void with_shift(int shift, F f) {
 
 // Entries are raised to this where 0 times -inf would not be a number: their weight stays 0.  Plain arithmetic holds where a tile's largest entry is far above it
 // and the exponents' scale keeps it finite.
-constexpr float kLow = -1e30f, kPlainEntry = 1e28f, kPlainScale = 1e6f;
+// (kLeastScale: below it an entry of kLow would have a weight.)
+constexpr float kLow = -1e30f, kPlainEntry = 1e28f, kPlainScale = 1e6f, kLeastScale = 1e-20f;
 
 template <typename T>
 struct Packed16;   // one word as entries
@@ -430,9 +431,12 @@ __device__ __forceinline__ float warp_sum_four(float a, float b, float c, float 
 
 // Exponents below this give weights of 0 and may be replaced by it.
 constexpr float kFarBelow = -1e30f;
+// The same where an exponent is multiplied by a gradient's factor, which is held to kMostFactor: their product stays finite, so that a weight of 0 makes it 0.
+constexpr float kNoWeight = -1e4f, kMostFactor = 1e33f;
+__device__ __forceinline__ float held_to(float v, float most) { return fminf(fmaxf(v, -most), most); }
 
 // What m k loses when it is rounded: plain tiles take their weights relative to the rounded m k, the others to m k itself.
-__device__ __forceinline__ bool plain_tile(float m, float k) { return fabsf(m) < kPlainEntry && k < kPlainScale; }
+__device__ __forceinline__ bool plain_tile(float m, float k) { return fabsf(m) < kPlainEntry && k < kPlainScale && k > kLeastScale; }
 __device__ __forceinline__ float rounded_off(float m, float k) { return plain_tile(m, k) ? fmaf(m, k, -(m * k)) : 0.0f; }
 
 }  // namespace tiles

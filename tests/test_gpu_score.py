@@ -370,3 +370,30 @@ def test_a_step_that_returns_log_probabilities(rsd, number):
     g = torch.ones(draft.shape[:2]).cuda()
     got = rsd.rsd_row_divergence_backward(draft, target, g)["grad_draft"]
     sc.check_gradient(got, *sc.divergence_gradient(draft, target, g, None, 1.0, 1.0), "gradient of the drafter's rows")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [1e-9, 1e-5, 1e10, 1e25, 1e35])
+def test_masked_entries_at_extreme_temperatures_and_weights(rsd, dtype, T):
+    """Masked entries keep weight 0 however flat the rest is, and get a gradient of 0 however large the factors are."""
+    V = 3001
+    rows = sc.random_rows((2, 2, V), DT[dtype], 2.0, 5)
+    rows[0, 0, ::2] = NEG
+    rows[1, 0, 100:] = NEG
+    rows[1, 1, 5:2500] = torch.finfo(DT[dtype]).min if T == 1e-5 else NEG
+    token = torch.tensor([[[1, 4, 1]] * 2] * 2, dtype=torch.int32).cuda()
+    out = rsd.rsd_token_logprobs(rows, token, top_k=3, temperature=T)
+    sc.check_scores(out, rows, token, 3, T)
+    g = torch.tensor([[[1.0, 2.0, -0.5]] * 2] * 2).cuda()
+    for size in (1.0, 1e9):
+        h = torch.full((2, 2), size).cuda()
+        got = rsd.rsd_token_logprobs_backward(rows, token, g, h, temperature=T)["grad_rows"]
+        sc.check_gradient(got, *sc.score_gradient(rows, token, g, h, T), "gradient")
+    target = (rows.float() + torch.where(rows > NEG, 1.0, 0.0) * sc.random_rows((2, 2, V), torch.float32, 0.5, 6)).to(DT[dtype])
+    near = rsd.rsd_row_divergence(rows, target, draft_temperature=T, target_temperature=T)
+    for k, (want, tol) in ((k, sc.divergences(rows, target, T, T)[k]) for k in ("kl", "reverse_kl", "overlap")):
+        if T > 1e-4 or k == "overlap":                           # (colder, a divergence is made of differences of 1e5 and more)
+            sc.close(near[k], want, tol, k)
+    for size in (1.0, 1e9):
+        h = torch.full((2, 2), size).cuda()
+        assert torch.isfinite(rsd.rsd_row_divergence_backward(rows, target, h, h, draft_temperature=T, target_temperature=T)["grad_draft"][rows == NEG]).all()
