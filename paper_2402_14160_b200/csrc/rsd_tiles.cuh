@@ -82,15 +82,6 @@ struct Packed16<float> {
             a = max_nan(a, max_nan(max_nan(__uint_as_float(w[k].x), __uint_as_float(w[k].y)), max_nan(__uint_as_float(w[k].z), __uint_as_float(w[k].w))));
         return a;
     }
-    template <int KW>
-    __device__ static __forceinline__ float smallest(const uint4 (&w)[KW]) {
-        float a = fminf(__uint_as_float(w[0].x), __uint_as_float(w[0].y));
-        a = fminf(a, fminf(__uint_as_float(w[0].z), __uint_as_float(w[0].w)));
-#pragma unroll
-        for (int k = 1; k < KW; ++k)
-            a = fminf(a, fminf(fminf(__uint_as_float(w[k].x), __uint_as_float(w[k].y)), fminf(__uint_as_float(w[k].z), __uint_as_float(w[k].w))));
-        return a;
-    }
     __device__ static __forceinline__ uint32_t raised_entry(uint32_t u) { return __float_as_uint(fmaxf(__uint_as_float(u), kLow)); }
     __device__ static __forceinline__ uint4 raised(const uint4& w) { return make_uint4(raised_entry(w.x), raised_entry(w.y), raised_entry(w.z), raised_entry(w.w)); }
     // whether one of two words has an entry above kLow where the other has none
@@ -143,24 +134,12 @@ struct Packed16<__nv_bfloat16> {
         w.x = clean_entry(w.x, bad), w.y = clean_entry(w.y, bad), w.z = clean_entry(w.z, bad), w.w = clean_entry(w.w, bad);
     }
     __device__ static __forceinline__ uint4 masked() { return make_uint4(kMasked, kMasked, kMasked, kMasked); }
-    __device__ static __forceinline__ uint32_t min2(uint32_t a, uint32_t b) {
-        uint32_t r;
-        asm("min.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-        return r;
-    }
     template <int KW>
     __device__ static __forceinline__ float largest(const uint4 (&w)[KW]) {
         uint32_t a = bf162_max_nan(bf162_max_nan(w[0].x, w[0].y), bf162_max_nan(w[0].z, w[0].w));
 #pragma unroll
         for (int k = 1; k < KW; ++k) a = bf162_max_nan(a, bf162_max_nan(bf162_max_nan(w[k].x, w[k].y), bf162_max_nan(w[k].z, w[k].w)));
         return max_nan(__uint_as_float(a << 16), __uint_as_float(a & 0xFFFF0000u));
-    }
-    template <int KW>
-    __device__ static __forceinline__ float smallest(const uint4 (&w)[KW]) {
-        uint32_t a = min2(min2(w[0].x, w[0].y), min2(w[0].z, w[0].w));
-#pragma unroll
-        for (int k = 1; k < KW; ++k) a = min2(a, min2(min2(w[k].x, w[k].y), min2(w[k].z, w[k].w)));
-        return fminf(__uint_as_float(a << 16), __uint_as_float(a & 0xFFFF0000u));
     }
     static constexpr uint32_t kLow2 = 0xF149F149u;   // kLow rounded to this type, twice
     __device__ static __forceinline__ uint32_t raised_entry(uint32_t u) {
