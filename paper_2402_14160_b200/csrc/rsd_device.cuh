@@ -93,6 +93,11 @@ __device__ __forceinline__ float max_nan(float a, float b) {  // NaN if either i
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
     return r;
 }
+__device__ __forceinline__ float min_nan(float a, float b) {
+    float r;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
 
 __device__ __forceinline__ uint4 ld_stream(const void* p) {
     uint4 v;

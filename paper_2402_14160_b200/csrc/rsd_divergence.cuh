@@ -259,7 +259,7 @@ __device__ __forceinline__ int status_of(const Result& r, bool bad) {
 
 // The divergences themselves in 64 bits: logarithms of sums cancel against each other.
 __device__ __forceinline__ float divergence_of(float d, float s, float other) {
-    return fmaxf((float)(0.693147180559945309 * ((double)d / (double)s + log2((double)other / (double)s))), 0.0f);
+    return max_nan((float)(0.693147180559945309 * ((double)d / (double)s + log2((double)other / (double)s))), 0.0f);
 }
 
 // log2 of a row's probabilities: v k - c + off in a plain row, (v - m) k - c otherwise; off is what c loses when it is rounded.
@@ -341,7 +341,7 @@ __global__ void __launch_bounds__(NW * 32, 32 / NW) divergence_kernel(const __gr
             float s = 0.0f;
             for (int t = lane; t < w.n_tiles; t += 32) s += w.sums[t].overlap;
             s = tiles::warp_sum_two(s, 0.0f, lane);
-            if (lane == 0) a.out_overlap[w.slot] = res.empty ? 0.0f : fminf(s * ex2_approx(p.off), 1.0f);
+            if (lane == 0) a.out_overlap[w.slot] = res.empty ? 0.0f : min_nan(s * ex2_approx(p.off), 1.0f);
         }
     }
     grid_started();

@@ -385,7 +385,7 @@ __global__ void __launch_bounds__(NW * 32, 32 / NW) score_rows_kernel(const __gr
         for (int i = n + tid; i < a.K; i += NW * 32) a.out_top_token[slot * a.K + i] = -1, a.out_top_logprob[slot * a.K + i] = kNegInf;
     }
     if (tid == 0) {
-        if (a.out_entropy) a.out_entropy[slot] = none ? 0.0f : fmaxf(lnz - 0.69314718f * __fdividef(total.w, total.s), 0.0f);
+        if (a.out_entropy) a.out_entropy[slot] = none ? 0.0f : max_nan(lnz - 0.69314718f * __fdividef(total.w, total.s), 0.0f);
         a.status[slot] = status_of_row | (there && none ? RSD_ST_EMPTY_ROW : 0) | (few ? RSD_ST_FEWER_THAN_K : 0);
     }
     grid_started();

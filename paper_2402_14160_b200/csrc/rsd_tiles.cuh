@@ -45,9 +45,9 @@ __device__ __forceinline__ void with_shift(int shift, F f) {
 }
 
 // Entries are raised to this where 0 times -inf would not be a number: their weight stays 0.  Plain arithmetic holds where a tile's largest entry is far above it
-// and the exponents' scale keeps it finite.
+// and the exponents' scale keeps it finite, and where the product of both is so small that it loses no more than half when it is rounded (see plain_tile).
 // (kLeastScale: below it an entry of kLow would have a weight.)
-constexpr float kLow = -1e30f, kPlainEntry = 1e28f, kPlainScale = 1e6f, kLeastScale = 1e-20f;
+constexpr float kLow = -1e30f, kPlainProduct = 16777216.0f, kPlainScale = 1e6f, kLeastScale = 1e-20f;
 
 template <typename T>
 struct Packed16;   // one word as entries
@@ -414,8 +414,9 @@ constexpr float kFarBelow = -1e30f;
 constexpr float kNoWeight = -1e4f, kMostFactor = 1e33f;
 __device__ __forceinline__ float held_to(float v, float most) { return fminf(fmaxf(v, -most), most); }
 
-// What m k loses when it is rounded: plain tiles take their weights relative to the rounded m k, the others to m k itself.
-__device__ __forceinline__ bool plain_tile(float m, float k) { return fabsf(m) < kPlainEntry && k < kPlainScale && k > kLeastScale; }
+// What m k loses when it is rounded: plain tiles take their weights relative to the rounded m k, the others to m k itself (m subtracted first).  Half a step of m k is 0.5 at
+// the most below 2^24, so that a plain tile's weights reach 2^0.5; at 2^31 it would be 64, and the largest weight infinite or 0.
+__device__ __forceinline__ bool plain_tile(float m, float k) { return fabsf(m) * k < kPlainProduct && k < kPlainScale && k > kLeastScale; }
 __device__ __forceinline__ float rounded_off(float m, float k) { return plain_tile(m, k) ? fmaf(m, k, -(m * k)) : 0.0f; }
 
 }  // namespace tiles
