@@ -345,6 +345,7 @@ int rsd_emitted_logprobs(const rsd_rows* target, int B, int num_nodes, int V, in
  *   ( sum_{t: token_t = x} g_t - p_x (sum_t g_t + h (ln p_x + H)) ) / T
  * The normalisers are taken from the row again, so that nothing has to be kept from the forward call.  A token given twice counts twice,
  * an absent one not at all; entries without probability get what the formula gives at p_x = 0; a row without entries gets 0 throughout.
+ * A weight of a token that is there, or of the entropy, that is NaN or infinite leaves no finite entry in its row's gradient; finite ones count in full.
  *   rows [B][R][V];  token [B][R][T], 1 <= T <= RSD_MAX_K;  grad_logprob [B][R][T], grad_entropy optional [B][R], fp32
  *   grad_rows    [B][R][V] dense, the rows' element type, rounded once; may not overlap the rows
  *   status       [B][R]
@@ -370,7 +371,8 @@ int rsd_row_divergence(const rsd_rows* draft, const rsd_rows* target, int B, int
  * Gradient of  grad_kl[b][r] KL(q||p) + grad_reverse_kl[b][r] KL(p||q)  with respect to the stored values of the draft rows:
  *   ( g (p_x - q_x) + h p_x (ln p_x - ln q_x - KL(p||q)) ) / T_draft
  * (either may be NULL, not both).  A row whose KL(p||q) is infinite gets no gradient of it (RSD_ST_ZERO_TARGET_PROB); a pair of rows of
- * which one has no entry gets 0 (RSD_ST_EMPTY_ROW).  status [B][R].
+ * which one has no entry gets 0 (RSD_ST_EMPTY_ROW).  Otherwise a weight that is NaN or infinite leaves no finite entry in its row's gradient; finite ones count in full.
+ * status [B][R].
  *   grad_draft   [B][R][V] dense, the rows' element type, rounded once; may not overlap the rows
  */
 int rsd_row_divergence_backward(const rsd_rows* draft, const rsd_rows* target, int B, int R, int V, const float* grad_kl,

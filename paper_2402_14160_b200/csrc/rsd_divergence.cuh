@@ -347,6 +347,30 @@ __global__ void __launch_bounds__(NW * 32, 32 / NW) divergence_kernel(const __gr
     grid_started();
 }
 
+// The gradient of rows that are not plain, or where products of weights and factors might leave fp32's range, in 64 bits: a weight of 0 makes every finite factor 0, and
+// factors that are not finite reach every entry.
+struct WideSlope {
+    float mp, mq, kp, kq, cp, cq;                  // log2 p = (v - mp) kp - cp, but for what the logarithms lost
+    double g, h, scale_p, scale_q, off, reverse;   // weights over the temperature, what the logarithms lost, KL(p||q)
+};
+template <typename T, bool REVERSE>
+__device__ __noinline__ void write_wide(const void* draft, const void* target, void* grad, int first, int step, int V, WideSlope f) {
+    auto entry = [](const void* row, int x) {      // -inf where it is none
+        const float v = RowIO<T>::scalar(row, x);
+        return v < __builtin_huge_valf() ? v : kNegInf;
+    };
+    for (int i = first; i < V; i += step) {
+        float x = fmaf(entry(draft, i) - f.mp, f.kp, -f.cp), u = fmaf(entry(target, i) - f.mq, f.kq, -f.cq);
+        const double wp = (double)ex2_approx(x) * f.scale_p, wq = (double)ex2_approx(u) * f.scale_q;
+        double slope = (wp - wq) * f.g;
+        if (REVERSE) {
+            x = fmaxf(x, tiles::kNoWeight), u = fmaxf(u, tiles::kNoWeight);
+            slope += wp * f.h * (0.693147180559945309 * ((double)x - (double)u + f.off) - f.reverse);
+        }
+        tiles::Packed16<T>::store(grad, i, (float)slope);
+    }
+}
+
 // d KL(q||p) / dv_x = (p_x - q_x) / T,   d KL(p||q) / dv_x = p_x (log p_x - log q_x - KL(p||q)) / T,   v the draft row, T its temperature.
 // A row whose KL(p||q) is infinite has no gradient of it.  Words of the gradient are written on their own 16-byte boundaries.
 //
@@ -369,18 +393,34 @@ __global__ void __launch_bounds__(NW * 32, 24 / NW) divergence_grad_kernel(const
     const float scale_p = ex2_approx(lp.off), scale_q = ex2_approx(lq.off);
     // gt (p - q) + p ht (ln 2 (log2 p - log2 q) - KL(p||q)); rows that are equal give 0
     const float reverse = REVERSE && ht != 0.0f ? 0.69314718f * (__fdividef(sm.total.dp, sm.total.sp) + res.log2_sq - res.log2_sp) : 0.0f;
-    const float c1f = ht * 0.69314718f, c0f = fmaf(c1f, lp.off - lq.off, -ht * reverse);
-    const unsigned long long c0 = tiles::both(tiles::held_to(c0f * scale_p, 1e38f)), c1 = tiles::both(tiles::held_to(c1f * scale_p, tiles::kMostFactor)),
-                             cg = tiles::both(tiles::held_to(gt * scale_p, 1e38f)), minus_ratio = tiles::both(-__fdividef(scale_q, scale_p)),
-                             minus_one = tiles::both(-1.0f);
+    const float c1f = ht * 0.69314718f * scale_p, c0f = fmaf(ht * 0.69314718f, lp.off - lq.off, -ht * reverse) * scale_p, cgf = gt * scale_p;
     char* const grad = (char*)a.grad + w.slot * a.V * (int64_t)sizeof(T);
     const int head = ALIGNED ? 0 : (int)((uintptr_t)grad & 15u) / (int)sizeof(T);   // entries between the boundary and the gradient's first one
-    auto word = [&](const uint4& pw, const uint4& qw, auto plain) {
-        constexpr bool PLAIN = decltype(plain)::value;
+    auto finish = [&] {
+        if (w.rank == 0 && tid == 0) {
+            Result said = res;
+            said.kl_infinite = false;                               // (its gradient is finite)
+            if (!REVERSE) said.reverse_infinite = false;
+            a.status[w.slot] = status_of(said, bad);
+        }
+        grid_started();
+    };
+    if (!res.empty && !(lp.plain && lq.plain && tiles::ordinary_factor(c0f) && tiles::ordinary_factor(c1f) && tiles::ordinary_factor(cgf))) {
+        WideSlope f;
+        f.mp = lp.plain ? 0.0f : sm.total.mp, f.mq = lq.plain ? 0.0f : sm.total.mq, f.kp = a.k_draft, f.kq = a.k_target, f.cp = lp.c, f.cq = lq.c;
+        f.g = (double)g * (double)a.inv_draft_temp, f.h = ht == 0.0f ? 0.0 : (double)h * (double)a.inv_draft_temp;
+        f.scale_p = (double)scale_p, f.scale_q = (double)scale_q, f.off = (double)lp.off - (double)lq.off, f.reverse = (double)reverse;
+        const int threads = NW * 32;
+        write_wide<T, REVERSE>(w.draft.base + w.draft.first, w.target.base + w.target.first, grad, (int)w.rank * threads + tid, (int)w.blocks * threads, a.V, f);
+        finish();
+        return;
+    }
+    const unsigned long long c0 = tiles::both(c0f), c1 = tiles::both(c1f), cg = tiles::both(cgf), minus_ratio = tiles::both(-__fdividef(scale_q, scale_p)), minus_one = tiles::both(-1.0f);
+    auto word = [&](const uint4& pw, const uint4& qw) {
         return P::make([&](int i) {
             float x, y, u, v;
-            split_f32x2(lp.of<PLAIN>(P::pair(pw, i)), x, y);
-            split_f32x2(lq.of<PLAIN>(P::pair(qw, i)), u, v);
+            split_f32x2(lp.of<true>(P::pair(pw, i)), x, y);
+            split_f32x2(lq.of<true>(P::pair(qw, i)), u, v);
             const unsigned long long wp = f32x2(ex2_approx(x), ex2_approx(y)), wq = f32x2(ex2_approx(u), ex2_approx(v));
             const unsigned long long apart = tiles::mul_f32x2(fma_f32x2(wq, minus_ratio, wp), cg);
             if (!REVERSE) return apart;
@@ -388,45 +428,35 @@ __global__ void __launch_bounds__(NW * 32, 24 / NW) divergence_grad_kernel(const
             return fma_f32x2(wp, fma_f32x2(fma_f32x2(f32x2(u, v), minus_one, f32x2(x, y)), c1, c0), apart);
         });
     };
-    auto write = [&](auto plain) {
-        // tiles of the gradient: `head` entries ahead of the rows'
+    // tiles of the gradient: `head` entries ahead of the rows'
 #pragma unroll 1
-        for (int t = last_tile(w, tiles::tiles_of<T>(head + a.V, kWords)); t >= 0; t -= w.step) {
-            const int x = t * kTile - head + lane * E;
-            char* const to = grad + (int64_t)x * (int)sizeof(T);
-            const bool whole = t * kTile >= head && (t + 1) * kTile - head <= a.V;
-            uint4 pw[kWords], qw[kWords];
-            tiles::load_words<T, ALIGNED, kWords, tiles::kReadLast>(pw, w.draft, x, whole, a.V);
-            tiles::load_words<T, ALIGNED, kWords, tiles::kReadLast>(qw, w.target, x, whole, a.V);
-            if (bad) {
-                bool ignored = false;
+    for (int t = last_tile(w, tiles::tiles_of<T>(head + a.V, kWords)); t >= 0; t -= w.step) {
+        const int x = t * kTile - head + lane * E;
+        char* const to = grad + (int64_t)x * (int)sizeof(T);
+        const bool whole = t * kTile >= head && (t + 1) * kTile - head <= a.V;
+        uint4 pw[kWords], qw[kWords];
+        tiles::load_words<T, ALIGNED, kWords, tiles::kReadLast>(pw, w.draft, x, whole, a.V);
+        tiles::load_words<T, ALIGNED, kWords, tiles::kReadLast>(qw, w.target, x, whole, a.V);
+        if (bad) {
+            bool ignored = false;
 #pragma unroll
-                for (int k = 0; k < kWords; ++k) P::clean(pw[k], ignored), P::clean(qw[k], ignored);
-            }
+            for (int k = 0; k < kWords; ++k) P::clean(pw[k], ignored), P::clean(qw[k], ignored);
+        }
 #pragma unroll
-            for (int k = 0; k < kWords; ++k) {
-                const int at = x + k * 32 * E;
-                if (!whole && (at >= a.V || at + E <= 0)) continue;
-                uint4 out = word(pw[k], qw[k], plain);
-                if (res.empty) out = make_uint4(0, 0, 0, 0);
-                if (whole || (at >= 0 && at + E <= a.V)) {
-                    __stcs((uint4*)(to + k * 512), out);
-                } else {
-                    for (int i = 0; i < E; ++i)
-                        if (at + i >= 0 && at + i < a.V) P::store(grad, at + i, P::get(out, i));
-                }
+        for (int k = 0; k < kWords; ++k) {
+            const int at = x + k * 32 * E;
+            if (!whole && (at >= a.V || at + E <= 0)) continue;
+            uint4 out = word(pw[k], qw[k]);
+            if (res.empty) out = make_uint4(0, 0, 0, 0);
+            if (whole || (at >= 0 && at + E <= a.V)) {
+                __stcs((uint4*)(to + k * 512), out);
+            } else {
+                for (int i = 0; i < E; ++i)
+                    if (at + i >= 0 && at + i < a.V) P::store(grad, at + i, P::get(out, i));
             }
         }
-    };
-    if (lp.plain && lq.plain) write(std::true_type());
-    else write(std::false_type());
-    if (w.rank == 0 && tid == 0) {
-        Result said = res;
-        said.kl_infinite = false;                                   // (its gradient is finite)
-        if (!REVERSE) said.reverse_infinite = false;
-        a.status[w.slot] = status_of(said, bad);
     }
-    grid_started();
+    finish();
 }
 
 }  // namespace divergence

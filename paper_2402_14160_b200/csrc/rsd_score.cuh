@@ -399,22 +399,43 @@ __global__ void __launch_bounds__(NW * 32, 32 / NW) score_rows_kernel(const __gr
 // are the limits under which masked entries get 0 whatever the factors).  Three rows an SM are what
 // shared memory holds, 24 warps; two exponentials an entry keep the special-function unit 60 % busy, and the warps wait for each other at the two barriers (15 % of
 // the stalls) and for the unit's queue.  Slower: blocks that stay for several rows and ask for the next one early (224: without arithmetic 180 against 159), 4 warps a row (225).
-struct Slope {                     // gradient of an entry without a token: p (c0 + c1 log2 p),   log2 p = v k - c (plain rows) or (v - m) k - c
+struct Slope {                     // gradient of an entry without a token: p (c0 + c1 log2 p),   log2 p = (v - m) k - c, m = 0 in a plain row
     float m, c, c0, c1, inv_temp;
+    double wide_c0, wide_c1;       // the factors of rows that are not plain, or where products in fp32 might leave its range
     int plain, none;
 };
 __device__ __forceinline__ Slope slope_of(const RowTotals& total, float G, float h, float inv_temp, float k) {
     Slope f;
-    f.m = total.m, f.inv_temp = inv_temp;
-    f.none = total.m == kNegInf, f.plain = tiles::plain_tile(total.m, k);
+    f.inv_temp = inv_temp;
+    f.none = total.m == kNegInf;
+    const bool plain = f.none || tiles::plain_tile(total.m, k);
+    f.m = plain ? 0.0f : total.m;
     const float log2s = f.none ? 0.0f : log2f(total.s), H = f.none ? 0.0f : 0.69314718f * (log2s - __fdividef(total.w, total.s));
     // what c loses when it is rounded goes into the factors
-    f.c = f.plain ? fmaf(total.m, k, log2s) : log2s;
-    const float off = f.plain ? -(fmaf(total.m, k, -f.c) + log2s) : 0.0f, scale = ex2_approx(off);
+    f.c = plain && !f.none ? fmaf(total.m, k, log2s) : log2s;
+    const float off = plain && !f.none ? -(fmaf(total.m, k, -f.c) + log2s) : 0.0f, scale = ex2_approx(off);
     f.c1 = f.none ? 0.0f : -h * 0.69314718f * inv_temp;
     f.c0 = f.none ? 0.0f : fmaf(f.c1, off, -(G + h * H) * inv_temp) * scale;
-    f.c0 = tiles::held_to(f.c0, 1e38f), f.c1 = tiles::held_to(f.c1 * scale, tiles::kMostFactor);
+    f.c1 *= scale;
+    f.plain = plain && tiles::ordinary_factor(f.c0) && tiles::ordinary_factor(f.c1);
+    if (!f.plain) {
+        const double c1 = -(double)h * 0.693147180559945309 * (double)inv_temp;
+        f.wide_c0 = (c1 * (double)off - ((double)G + (double)h * (double)H) * (double)inv_temp) * (double)scale;
+        f.wide_c1 = c1 * (double)scale;
+    }
     return f;
+}
+// The gradient of an entry in 64 bits, and of a row's entries from..to - 1: a weight of 0 makes every finite factor 0, and factors that are not finite reach every entry.
+template <bool ENTROPY>
+__device__ __forceinline__ double wide_slope(float v, float k, const Slope& f) {
+    float x = fmaf(v - f.m, k, -f.c);
+    if (ENTROPY) x = fmaxf(x, tiles::kNoWeight);
+    const double p = (double)ex2_approx(x);
+    return p * (ENTROPY ? fma((double)x, f.wide_c1, f.wide_c0) : f.wide_c0);
+}
+template <typename T, bool ENTROPY>
+__device__ __noinline__ void write_wide(const void* row, void* grad, int from, int to, float k, const Slope& f) {
+    for (int x = from + (int)threadIdx.x; x < to; x += (int)blockDim.x) tiles::Packed16<T>::store(grad, x, (float)wide_slope<ENTROPY>(entry<T>(row, x), k, f));
 }
 
 template <typename T, bool ALIGNED, bool ENTROPY, int NW>
@@ -481,69 +502,80 @@ __global__ void __launch_bounds__(NW * 32, 24 / NW) score_grad_kernel(const __gr
     const Slope f = slope_of_row;
     bad = status_of_row & RSD_ST_NAN_INPUT;
     char* const grad = (char*)a.grad + (int64_t)slot * a.V * (int64_t)sizeof(T);
-    const unsigned long long minus_m = tiles::both(f.none || f.plain ? 0.0f : -f.m), kk = tiles::both(a.k), minus_c = tiles::both(-f.c), c0 = tiles::both(f.c0), c1 = tiles::both(f.c1);
-    auto slope = [&](unsigned long long v, auto plain_row) {
+    if (!f.plain) {
+        const int from = t0 * kTile, to = min(t1 * kTile, a.V);
+        write_wide<T, ENTROPY>(row, grad, from, to, a.k, slope_of_row);
+        __syncthreads();
+        const int32_t mine = warp == 0 && lane < a.T ? tokens[lane] : -1;
+        if (mine >= from && mine < to) {           // (as below)
+            double own = wide_slope<ENTROPY>(entry<T>(row, mine), a.k, f);
+            bool first = true;
+            for (int i = 0; i < a.T; ++i)
+                if (tokens[i] == mine) own = fma((double)weights[i], (double)f.inv_temp, own), first = first && i >= lane;
+            if (first) P::store(grad, mine, (float)own);
+        }
+        grid_started();
+        return;
+    }
+    const unsigned long long kk = tiles::both(a.k), minus_c = tiles::both(-f.c), c0 = tiles::both(f.c0), c1 = tiles::both(f.c1);
+    auto slope = [&](unsigned long long v) {
         float x, y;
-        const unsigned long long l = fma_f32x2(decltype(plain_row)::value ? v : add_f32x2(v, minus_m), kk, minus_c);
+        const unsigned long long l = fma_f32x2(v, kk, minus_c);
         split_f32x2(l, x, y);
         if (ENTROPY) x = fmaxf(x, tiles::kNoWeight), y = fmaxf(y, tiles::kNoWeight);
         const unsigned long long p = f32x2(ex2_approx(x), ex2_approx(y));
         return tiles::mul_f32x2(p, ENTROPY ? fma_f32x2(f32x2(x, y), c1, c0) : c0);
     };
     const int head = ALIGNED ? 0 : (int)((uintptr_t)grad & 15u) / (int)sizeof(T);   // entries between the boundary and the gradient's first one
-    auto word = [&](const uint4& v, auto plain_row) {
-        return P::make([&](int i) { return slope(P::pair(v, i), plain_row); });
+    auto word = [&](const uint4& v) {
+        return P::make([&](int i) { return slope(P::pair(v, i)); });
     };
-    auto write = [&](auto plain_row) {
-        const int last = t1 == n_tiles ? tiles::tiles_of<T>(head + a.V, kWords) : t1;   // tiles of the gradient: `head` entries ahead of the row's
+    const int last = t1 == n_tiles ? tiles::tiles_of<T>(head + a.V, kWords) : t1;   // tiles of the gradient: `head` entries ahead of the row's
 #pragma unroll 1
-        for (int t = t0 + warp; t < last && t0 < t1; t += NW) {
-            const int x = t * kTile - head + lane * E;
-            char* const to = grad + (int64_t)x * (int)sizeof(T);
-            const bool whole = t * kTile >= head && (t + 1) * kTile - head <= a.V;
-            uint4 w[kWords];
-            tiles::held_words<T, ALIGNED, kWords>(w, held, view, t0, t1, x, a.V);
-            if (bad) {
-                bool ignored = false;
+    for (int t = t0 + warp; t < last && t0 < t1; t += NW) {
+        const int x = t * kTile - head + lane * E;
+        char* const to = grad + (int64_t)x * (int)sizeof(T);
+        const bool whole = t * kTile >= head && (t + 1) * kTile - head <= a.V;
+        uint4 w[kWords];
+        tiles::held_words<T, ALIGNED, kWords>(w, held, view, t0, t1, x, a.V);
+        if (bad) {
+            bool ignored = false;
 #pragma unroll
-                for (int k = 0; k < kWords; ++k) P::clean(w[k], ignored);
-            }
-            if (whole) {
+            for (int k = 0; k < kWords; ++k) P::clean(w[k], ignored);
+        }
+        if (whole) {
 #pragma unroll
-                for (int k = 0; k < kWords; ++k) __stcs((uint4*)(to + k * 512), word(w[k], plain_row));
-            } else {
+            for (int k = 0; k < kWords; ++k) __stcs((uint4*)(to + k * 512), word(w[k]));
+        } else {
 #pragma unroll
-                for (int k = 0; k < kWords; ++k) {
-                    const int at = x + k * 32 * E;
-                    if (at >= 0 && at + E <= a.V) {
-                        __stcs((uint4*)(to + k * 512), word(w[k], plain_row));
-                    } else if (at + E > 0 && at < a.V) {
-                        const uint4 g = word(w[k], plain_row);
-                        for (int i = 0; i < E; ++i)
-                            if (at + i >= 0 && at + i < a.V) P::store(grad, at + i, P::get(g, i));
-                    }
-                }
-            }
-            __syncwarp();
-            // The entries of the tokens in this tile again, with their weights: a token given twice has both, and its first lane stores it.
-            const int32_t mine = lane < a.T ? tokens[lane] : -1;
-            if (mine >= 0 && (mine + head) / kTile == t) {
-                float own = 0.0f;
-                bool first = true;
-                for (int i = 0; i < a.T; ++i)
-                    if (tokens[i] == mine) own += weights[i], first = first && i >= lane;
-                if (first) {
-                    const int at = view.first + mine * (int)sizeof(T) - t0 * kWords * 512, tile = min(at / (kWords * 512), t1 - t0 - 1);
-                    const float v = at >= 0 ? entry<T>(dynamic_bytes + at + tile * 16, 0) : entry<T>(view.base + view.first, mine);
-                    float rest, ignored;
-                    split_f32x2(slope(tiles::both(v), plain_row), rest, ignored);
-                    P::store(grad, mine, f.none ? 0.0f : fmaf(own, f.inv_temp, rest));
+            for (int k = 0; k < kWords; ++k) {
+                const int at = x + k * 32 * E;
+                if (at >= 0 && at + E <= a.V) {
+                    __stcs((uint4*)(to + k * 512), word(w[k]));
+                } else if (at + E > 0 && at < a.V) {
+                    const uint4 g = word(w[k]);
+                    for (int i = 0; i < E; ++i)
+                        if (at + i >= 0 && at + i < a.V) P::store(grad, at + i, P::get(g, i));
                 }
             }
         }
-    };
-    if (f.plain) write(std::true_type());
-    else write(std::false_type());
+        __syncwarp();
+        // The entries of the tokens in this tile again, with their weights: a token given twice has both, and its first lane stores it.
+        const int32_t mine = lane < a.T ? tokens[lane] : -1;
+        if (mine >= 0 && (mine + head) / kTile == t) {
+            float own = 0.0f;
+            bool first = true;
+            for (int i = 0; i < a.T; ++i)
+                if (tokens[i] == mine) own += weights[i], first = first && i >= lane;
+            if (first) {
+                const int at = view.first + mine * (int)sizeof(T) - t0 * kWords * 512, tile = min(at / (kWords * 512), t1 - t0 - 1);
+                const float v = at >= 0 ? entry<T>(dynamic_bytes + at + tile * 16, 0) : entry<T>(view.base + view.first, mine);
+                float rest, ignored;
+                split_f32x2(slope(tiles::both(v)), rest, ignored);
+                P::store(grad, mine, f.none ? 0.0f : fmaf(own, f.inv_temp, rest));
+            }
+        }
+    }
     grid_started();
 }
 

@@ -410,9 +410,10 @@ __device__ __forceinline__ float warp_sum_four(float a, float b, float c, float 
 
 // Exponents below this give weights of 0 and may be replaced by it.
 constexpr float kFarBelow = -1e30f;
-// The same where an exponent is multiplied by a gradient's factor, which is held to kMostFactor: their product stays finite, so that a weight of 0 makes it 0.
+// The same where an exponent is multiplied by a gradient's factor of at most kMostFactor: their product stays finite, so that a weight of 0 makes it 0.  Rows with larger factors, and
+// with factors that are not finite, are written in 64 bits.
 constexpr float kNoWeight = -1e4f, kMostFactor = 1e33f;
-__device__ __forceinline__ float held_to(float v, float most) { return fminf(fmaxf(v, -most), most); }
+__device__ __forceinline__ bool ordinary_factor(float v) { return fabsf(v) <= kMostFactor; }   // (NaN is none)
 
 // What m k loses when it is rounded: plain tiles take their weights relative to the rounded m k, the others to m k itself (m subtracted first).  Half a step of m k is 0.5 at
 // the most below 2^24, so that a plain tile's weights reach 2^0.5; at 2^31 it would be 64, and the largest weight infinite or 0.
