@@ -364,7 +364,7 @@ __device__ __noinline__ void write_wide(const void* draft, const void* target, v
         const double wp = (double)ex2_approx(x) * f.scale_p, wq = (double)ex2_approx(u) * f.scale_q;
         double slope = (wp - wq) * f.g;
         if (REVERSE) {
-            x = fmaxf(x, tiles::kNoWeight), u = fmaxf(u, tiles::kNoWeight);
+            x = fmaxf(x, tiles::kLowest), u = fmaxf(u, tiles::kLowest);
             slope += wp * f.h * (0.693147180559945309 * ((double)x - (double)u + f.off) - f.reverse);
         }
         tiles::Packed16<T>::store(grad, i, (float)slope);
@@ -424,8 +424,10 @@ __global__ void __launch_bounds__(NW * 32, 24 / NW) divergence_grad_kernel(const
             const unsigned long long wp = f32x2(ex2_approx(x), ex2_approx(y)), wq = f32x2(ex2_approx(u), ex2_approx(v));
             const unsigned long long apart = tiles::mul_f32x2(fma_f32x2(wq, minus_ratio, wp), cg);
             if (!REVERSE) return apart;
-            x = fmaxf(x, tiles::kNoWeight), y = fmaxf(y, tiles::kNoWeight), u = fmaxf(u, tiles::kNoWeight), v = fmaxf(v, tiles::kNoWeight);
-            return fma_f32x2(wp, fma_f32x2(fma_f32x2(f32x2(u, v), minus_one, f32x2(x, y)), c1, c0), apart);
+            x = fmaxf(x, tiles::kLowest), y = fmaxf(y, tiles::kLowest), u = fmaxf(u, tiles::kLowest), v = fmaxf(v, tiles::kLowest);
+            // (the weight first: the target's logarithm may be as low as it likes where the draft has mass, and is of no account where it has none)
+            const unsigned long long far = tiles::mul_f32x2(wp, fma_f32x2(f32x2(u, v), minus_one, f32x2(x, y)));
+            return fma_f32x2(far, c1, fma_f32x2(wp, c0, apart));
         });
     };
     // tiles of the gradient: `head` entries ahead of the rows'

@@ -408,8 +408,8 @@ __device__ __forceinline__ float warp_sum_four(float a, float b, float c, float 
     return mine;
 }
 
-// Exponents below this give weights of 0 and may be replaced by it.
-constexpr float kFarBelow = -1e30f;
+// Exponents below this give weights of 0 and may be replaced by it; kLowest: the lowest finite one, where the exponent itself counts.
+constexpr float kFarBelow = -1e30f, kLowest = -3.402823466e38f;
 // The same where an exponent is multiplied by a gradient's factor of at most kMostFactor: their product stays finite, so that a weight of 0 makes it 0.  Rows with larger factors, and
 // with factors that are not finite, are written in 64 bits.
 constexpr float kNoWeight = -1e4f, kMostFactor = 1e33f;
