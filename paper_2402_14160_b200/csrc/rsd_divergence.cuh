@@ -21,11 +21,15 @@ namespace divergence {
 
 constexpr int kWords = 4;
 
+// Sums of weight times difference are kept in units of 2^20: a difference may be anything that fp32 holds, and up to 262,144 of them are added.
+constexpr float kUnit = 1.0f / 1048576.0f;
+
 struct Sums {   // of a tile of both rows, relative to its largest entries; every block of the pair has those of all tiles
     float sp, sq, dp, dq, mp, mq, overlap, unused;
 };
 struct Totals {
-    float sp, sq, dp, dq, mp, mq;   // sums of weights, of weight times b - a (p), a - b (q), largest entries
+    float sp, sq, dp, dq, mp, mq;   // sums of weights, of weight times b - a (p), a - b (q), in units, largest entries
+    float alone_p, alone_q;         // largest entries of tiles that are missing in the other row
 };
 struct Smem {
     Totals total;
@@ -86,7 +90,7 @@ __device__ __noinline__ CarefulSums add_tile_careful(Words p, Words q, float mp,
             const float wp = ex2_approx(b), wq = ex2_approx(a), d = in_p && in_q ? a - b : 0.0f;
             if (in_q && !in_p) l.alone_q = fmaxf(l.alone_q, vq);
             if (in_p && !in_q) l.alone_p = fmaxf(l.alone_p, vp);
-            l.sp += wp, l.sq += wq, l.dp = fmaf(wp, d, l.dp), l.dq = fmaf(wq, d, l.dq);
+            l.sp += wp, l.sq += wq, l.dp = fmaf(wp, d * kUnit, l.dp), l.dq = fmaf(wq, d * kUnit, l.dq);
         }
     }
     return l;
@@ -107,17 +111,17 @@ __device__ __forceinline__ void tile_sums(uint4 (&p)[kWords], uint4 (&q)[kWords]
     LaneSums l = {tiles::both(0.0f), tiles::both(0.0f), tiles::both(0.0f), tiles::both(0.0f)};
     const bool plain = tiles::plain_tile(mp, kp) && tiles::plain_tile(mq, kq);
     float x, y, sp, sq, dp, dq;
-    auto halves = [&] {
+    auto halves = [&](float unit) {
         split_f32x2(l.sp, x, y), sp = x + y;
         split_f32x2(l.sq, x, y), sq = x + y;
-        split_f32x2(l.dp, x, y), dp = -(x + y);
-        split_f32x2(l.dq, x, y), dq = x + y;
+        split_f32x2(l.dp, x, y), dp = -(x + y) * unit;
+        split_f32x2(l.dq, x, y), dq = (x + y) * unit;
     };
     bool done = false;
     if (plain && !(BOTH && masked)) {
         add_tile<T, BOTH, false>(p, q, mp, mq, kp, kq, l);
-        halves();
-        done = !BOTH || !__any_sync(0xFFFFFFFFu, !(fabsf(dp + dq) < __builtin_huge_valf()));   // (an entry without mass gives 0 times infinity)
+        halves(kUnit);
+        done = !BOTH || !__any_sync(0xFFFFFFFFu, !(fabsf(dp + dq) < __builtin_huge_valf()));   // (an entry without mass gives 0 times infinity, one far below may give infinity)
     }
     if (!done) {
         masked = true;
@@ -127,6 +131,7 @@ __device__ __forceinline__ void tile_sums(uint4 (&p)[kWords], uint4 (&q)[kWords]
         if (BOTH && plain && __all_sync(0xFFFFFFFFu, alike)) {
             l = {tiles::both(0.0f), tiles::both(0.0f), tiles::both(0.0f), tiles::both(0.0f)};
             add_tile<T, BOTH, true>(p, q, mp, mq, kp, kq, l);
+            halves(kUnit);
         } else {
             Words pw, qw;
 #pragma unroll
@@ -134,8 +139,8 @@ __device__ __forceinline__ void tile_sums(uint4 (&p)[kWords], uint4 (&q)[kWords]
             const CarefulSums c = add_tile_careful<T>(pw, qw, mp, mq, kp, kq);
             l = {f32x2(c.sp, 0.0f), f32x2(c.sq, 0.0f), f32x2(c.dp, 0.0f), f32x2(c.dq, 0.0f)};
             alone_p = fmaxf(alone_p, c.alone_p), alone_q = fmaxf(alone_q, c.alone_q);
+            halves(1.0f);
         }
-        halves();
     }
     next();
     // Sums::sp, sq, dp, dq are in eight lanes each (without the last two in sixteen each); four lanes store them and two the largest entries, in every block.
@@ -156,21 +161,23 @@ __device__ __forceinline__ Totals join(const Sums* sums, int n, float kp, float 
     float mp = kNegInf, mq = kNegInf;
     for (int t = lane; t < n; t += 32) mp = fmaxf(mp, sums[t].mp), mq = fmaxf(mq, sums[t].mq);
     mp = tiles::warp_max_nan(mp), mq = tiles::warp_max_nan(mq);
-    float sp = 0.0f, sq = 0.0f, dp = 0.0f, dq = 0.0f;
+    float sp = 0.0f, sq = 0.0f, dp = 0.0f, dq = 0.0f, alone_p = kNegInf, alone_q = kNegInf;
     for (int t = lane; t < n; t += 32) {
-        const float mtp = sums[t].mp, mtq = sums[t].mq;
-        const bool has_p = mtp > kNegInf, has_q = mtq > kNegInf;
-        const float bp = has_p ? fmaxf((mtp - mp) * kp, tiles::kFarBelow) - tiles::rounded_off(mtp, kp) : 0.0f;
-        const float bq = has_q ? fmaxf((mtq - mq) * kq, tiles::kFarBelow) - tiles::rounded_off(mtq, kq) : 0.0f;
+        const float mtp = sums[t].mp, mtq = sums[t].mq, far_p = (mtp - mp) * kp, far_q = (mtq - mq) * kq;
+        const bool has_p = far_p > kNegInf, has_q = far_q > kNegInf;   // (a tile whose distance leaves fp32's range is missing, like single entries)
+        const float bp = has_p ? far_p - tiles::rounded_off(mtp, kp) : 0.0f, bq = has_q ? far_q - tiles::rounded_off(mtq, kq) : 0.0f;
+        if (has_p && !has_q) alone_p = fmaxf(alone_p, mtp);
+        if (has_q && !has_p) alone_q = fmaxf(alone_q, mtq);
         const float fp = has_p ? ex2_approx(bp) : 0.0f, fq = has_q ? ex2_approx(bq) : 0.0f;
         sp = fmaf(fp, sums[t].sp, sp), sq = fmaf(fq, sums[t].sq, sq);
         if (BOTH) {
-            const float d = has_p && has_q ? bq - bp : 0.0f;
+            const float d = has_p && has_q ? fmaxf(fminf(bq - bp, -tiles::kLowest), tiles::kLowest) * kUnit : 0.0f;
             dp = fmaf(fp, fmaf(-d, sums[t].sp, sums[t].dp), dp), dq = fmaf(fq, fmaf(d, sums[t].sq, sums[t].dq), dq);
         }
     }
     const float sum = tiles::warp_sum_four(sp, sq, dp, dq, lane);
-    return {__shfl_sync(0xFFFFFFFFu, sum, 0), __shfl_sync(0xFFFFFFFFu, sum, 8), __shfl_sync(0xFFFFFFFFu, sum, 16), __shfl_sync(0xFFFFFFFFu, sum, 24), mp, mq};
+    if (BOTH) alone_p = tiles::warp_max_nan(alone_p), alone_q = tiles::warp_max_nan(alone_q);
+    return {__shfl_sync(0xFFFFFFFFu, sum, 0), __shfl_sync(0xFFFFFFFFu, sum, 8), __shfl_sync(0xFFFFFFFFu, sum, 16), __shfl_sync(0xFFFFFFFFu, sum, 24), mp, mq, alone_p, alone_q};
 }
 
 // A pair of rows and the tiles of it that this warp has: tile t belongs to warp t / blocks mod NW of block t mod blocks.
@@ -227,7 +234,11 @@ __device__ __forceinline__ bool read_rows(const DivergenceArgs& a, const Pair& w
     tiles::row_barrier(w.blocks);
     if (warp == 0) {
         const Totals t = join<BOTH>(w.sums, w.n_tiles, a.k_draft, a.k_target, lane);
-        if (lane == 0) sm.total = t;
+        if (lane == 0) {
+            sm.total = t;
+            if (BOTH && t.alone_p > kNegInf) sm.alone_p = max(sm.alone_p, float_to_ordered(t.alone_p));
+            if (BOTH && t.alone_q > kNegInf) sm.alone_q = max(sm.alone_q, float_to_ordered(t.alone_q));
+        }
     }
     __syncthreads();
     return sm.status != 0;
@@ -259,7 +270,7 @@ __device__ __forceinline__ int status_of(const Result& r, bool bad) {
 
 // The divergences themselves in 64 bits: logarithms of sums cancel against each other.
 __device__ __forceinline__ float divergence_of(float d, float s, float other) {
-    return max_nan((float)(0.693147180559945309 * ((double)d / (double)s + log2((double)other / (double)s))), 0.0f);
+    return max_nan((float)(0.693147180559945309 * ((double)d / ((double)kUnit * (double)s) + log2((double)other / (double)s))), 0.0f);
 }
 
 // log2 of a row's probabilities: v k - c + off in a plain row, (v - m) k - c otherwise; off is what c loses when it is rounded.
@@ -392,7 +403,7 @@ __global__ void __launch_bounds__(NW * 32, 24 / NW) divergence_grad_kernel(const
     const LogProb lp = log_prob(sm.total.mp, a.k_draft, res.log2_sp, res.empty), lq = log_prob(sm.total.mq, a.k_target, res.log2_sq, res.empty);
     const float scale_p = ex2_approx(lp.off), scale_q = ex2_approx(lq.off);
     // gt (p - q) + p ht (ln 2 (log2 p - log2 q) - KL(p||q)); rows that are equal give 0
-    const float reverse = REVERSE && ht != 0.0f ? 0.69314718f * (__fdividef(sm.total.dp, sm.total.sp) + res.log2_sq - res.log2_sp) : 0.0f;
+    const float reverse = REVERSE && ht != 0.0f ? 0.69314718f * (__fdividef(sm.total.dp, sm.total.sp) * (1.0f / kUnit) + res.log2_sq - res.log2_sp) : 0.0f;
     const float c1f = ht * 0.69314718f * scale_p, c0f = fmaf(ht * 0.69314718f, lp.off - lq.off, -ht * reverse) * scale_p, cgf = gt * scale_p;
     char* const grad = (char*)a.grad + w.slot * a.V * (int64_t)sizeof(T);
     const int head = ALIGNED ? 0 : (int)((uintptr_t)grad & 15u) / (int)sizeof(T);   // entries between the boundary and the gradient's first one

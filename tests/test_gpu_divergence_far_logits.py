@@ -51,3 +51,43 @@ def test_gradient_at_low_entries_of_the_target(rsd, dtype, low):
     target[1, :, 1000:4000:3] = low
     draft[2, :, 17] = low                                       # and where neither has mass
     assert not _check(rsd, draft, target)["status"].any()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("low", [-1e20, -1e30, -5e30, -1e35, -1e38])
+@pytest.mark.parametrize("T", [1.0, 2.0])
+def test_tiles_of_one_row_masked_with_a_number(rsd, dtype, low, T):
+    """Whole tiles: their sums are relative to the mask, and their logarithms count in full."""
+    draft, target = _pair((5, 2, 5003), dtype)
+    target[0, :, :2048] = low
+    draft[1, :, 2048:] = low
+    target[2, :, 3000:] = low
+    target[2, :, 10:2000:7] = low
+    draft[3, :, 1024:4096], target[3, :, 1024:4096] = -1e9, low     # no mass in either, far apart
+    target[4, :, 1024:4096], draft[4, :, 1024:4096] = -1e4, low
+    assert not _check(rsd, draft, target, T, T)["status"].any()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_tiles_of_the_lowest_value(rsd, dtype):
+    """Beyond fp32's range in units of a factor 2 an entry is missing, whether its tile holds others or not."""
+    low = torch.finfo(DT[dtype]).min
+    zd, zt = rsd.ST_ZERO_DRAFT_PROB, rsd.ST_ZERO_TARGET_PROB
+    for places in (slice(0, 2048), slice(0, 5003, 2), slice(17, 18)):
+        draft, target = _pair((3, 2, 5003), dtype)
+        target[0, :, places] = low
+        draft[1, :, places] = low
+        draft[2, :, places], target[2, :, places] = low, low
+        out = rsd.rsd_row_divergence(draft, target)
+        assert out["status"].tolist() == [[zt] * 2, [zd] * 2, [0] * 2]
+        assert torch.isinf(out["reverse_kl"][0]).all() and torch.isinf(out["kl"][1]).all()
+        want = sc.divergences(draft, target, 1.0, 1.0)
+        for k, rows in (("kl", (0, 2)), ("reverse_kl", (1, 2)), ("overlap", (0, 1, 2))):
+            for r in rows:
+                sc.close(out[k][r], want[k][0][r], want[k][1][r], k)
+        g = torch.ones((3, 2)).cuda()
+        got = rsd.rsd_row_divergence_backward(draft, target, g, g)
+        assert got["status"].tolist() == [[zt] * 2, [0] * 2, [0] * 2]
+        alone = rsd.rsd_row_divergence_backward(draft, target, g)["grad_draft"]
+        assert torch.equal(got["grad_draft"][0], alone[0])
+        _check(rsd, draft, target, 2.0, 2.0)                    # (within the range)
