@@ -96,7 +96,7 @@ __device__ __noinline__ CarefulSums add_tile_careful(Words p, Words q, float mp,
     return l;
 }
 
-// masked: the row's last tile had entries without mass, so that this one is looked through for them at once.
+// masked: a tile of this warp had entries without mass, so that this one is looked through for them at once.
 // next() reads the warp's next tile into the words' places, ahead of the sums over the warp.
 template <typename T, bool BOTH, typename F>   // BOTH: the sums of weight times difference too
 __device__ __forceinline__ void tile_sums(uint4 (&p)[kWords], uint4 (&q)[kWords], float kp, float kq, int t, int lane, uint32_t blocks, Sums* sums, float& alone_p, float& alone_q,
@@ -117,18 +117,23 @@ __device__ __forceinline__ void tile_sums(uint4 (&p)[kWords], uint4 (&q)[kWords]
         split_f32x2(l.dp, x, y), dp = -(x + y) * unit;
         split_f32x2(l.dq, x, y), dq = (x + y) * unit;
     };
+    // Which form a tile is summed in depends on the tile alone (where the same entries have no mass in both rows the first two give the same bits).
+    auto alike = [&] {
+        bool same = true;
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) same = same && !P::differ(p[i], q[i]);
+        return __all_sync(0xFFFFFFFFu, same) != 0;
+    };
+    const bool known = BOTH && plain && masked && alike();
     bool done = false;
-    if (plain && !(BOTH && masked)) {
+    if (plain && !known) {
         add_tile<T, BOTH, false>(p, q, mp, mq, kp, kq, l);
         halves(kUnit);
         done = !BOTH || !__any_sync(0xFFFFFFFFu, !(fabsf(dp + dq) < __builtin_huge_valf()));   // (an entry without mass gives 0 times infinity, one far below may give infinity)
     }
     if (!done) {
         masked = true;
-        bool alike = true;
-#pragma unroll
-        for (int i = 0; i < kWords; ++i) alike = alike && !P::differ(p[i], q[i]);
-        if (BOTH && plain && __all_sync(0xFFFFFFFFu, alike)) {
+        if (BOTH && plain && (known || alike())) {
             l = {tiles::both(0.0f), tiles::both(0.0f), tiles::both(0.0f), tiles::both(0.0f)};
             add_tile<T, BOTH, true>(p, q, mp, mq, kp, kq, l);
             halves(kUnit);
