@@ -18,6 +18,22 @@ int check_batch(int B, int R) {
     if ((int64_t)B * R > 0x7FFFFFFF) return fail(RSD_ERR_UNSUPPORTED, "B * R too large");
     return RSD_OK;
 }
+// Whether `bytes` from `out` on lie over an entry of the rows [B][R][V]; memory between the rows is not theirs.
+bool over_rows(const rsd_rows* rows, int B, int R, int V, const void* out, int64_t bytes) {
+    typedef __int128 wide;                                       // (strides may be anything that 64 bits hold)
+    const int64_t elem = rows->dtype == RSD_F32 ? 4 : 2;
+    const wide lo = (wide)(uintptr_t)out - (wide)(uintptr_t)rows->data, hi = lo + bytes, row = (wide)V * elem;
+    const wide row_step = (wide)rows->row_stride * elem, seq_step = (wide)rows->seq_stride * elem;
+    const wide sequence = row_step * (R - 1) + row;              // from a sequence's first entry to behind its last
+    // of pieces of `length` bytes, one every `step` bytes, the first that ends behind `from`
+    const auto first = [](wide step, wide length, wide from) { return from < length || step == 0 ? (wide)0 : (from - length) / step + 1; };
+    for (wide b = first(seq_step, sequence, lo); b < B && b * seq_step < hi; ++b) {
+        const wide start = b * seq_step, r = first(row_step, row, lo - start), at = start + r * row_step;
+        if (r < R && at < hi && at + row > lo) return true;
+        if (seq_step == 0) break;
+    }
+    return false;
+}
 float inverse(float temp) { return (float)std::min(1.0 / (double)temp, 3.0e38); }
 float exponent_scale(float temp) { return (float)std::min(1.4426950408889634 / (double)temp, 3.0e38); }   // log2(e) / T
 bool dense_aligned(const void* p, int V, int dtype) { return (uintptr_t)p % 16 == 0 && (int64_t)V * (dtype == RSD_F32 ? 4 : 2) % 16 == 0; }
@@ -114,7 +130,7 @@ int rsd_token_logprobs_backward(const rsd_rows* rows, int B, int R, int V, const
     if (int e = check_batch(B, R)) return e;
     if (T < 1 || T > RSD_MAX_K) return fail(RSD_ERR_UNSUPPORTED, "T = %d outside [1, %d]", T, (int)RSD_MAX_K);
     if (!token || !grad_logprob || !grad_rows || !status) return fail(RSD_ERR_INVALID_ARG, "null argument");
-    if (grad_rows == rows->data) return fail(RSD_ERR_INVALID_ARG, "grad_rows may not overlap the rows");
+    if (over_rows(rows, B, R, V, grad_rows, (int64_t)B * R * V * (rows->dtype == RSD_F32 ? 4 : 2))) return fail(RSD_ERR_INVALID_ARG, "grad_rows may not overlap the rows");
     if (B == 0) return RSD_OK;
     cudaStream_t s = (cudaStream_t)stream;
     rsd::ScoreArgs a = score_args(rows, R, V, T, 0);
@@ -147,7 +163,8 @@ int rsd_row_divergence_backward(const rsd_rows* draft, const rsd_rows* target, i
     g_err[0] = 0;
     if (int e = check_pair(draft, target, B, R, V)) return e;
     if (!status || !grad_draft || (!grad_kl && !grad_reverse_kl)) return fail(RSD_ERR_INVALID_ARG, "null argument");
-    if (grad_draft == draft->data || grad_draft == target->data) return fail(RSD_ERR_INVALID_ARG, "grad_draft may not overlap the rows");
+    const int64_t bytes = (int64_t)B * R * V * (draft->dtype == RSD_F32 ? 4 : 2);
+    if (over_rows(draft, B, R, V, grad_draft, bytes) || over_rows(target, B, R, V, grad_draft, bytes)) return fail(RSD_ERR_INVALID_ARG, "grad_draft may not overlap the rows");
     if (B == 0) return RSD_OK;
     cudaStream_t s = (cudaStream_t)stream;
     rsd::DivergenceArgs a = divergence_args(draft, target, R, V);
