@@ -4,11 +4,12 @@
 // on attribute look-ups and conversions, more than a small draft or walk takes on the GPU; this takes two to three.
 #include <Python.h>
 #include <dlfcn.h>
-#include <ATen/ops/empty.h>
+#include <ATen/EmptyTensor.h>
 #include <torch/csrc/Device.h>
 #include <torch/csrc/DynamicTypes.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 
@@ -324,13 +325,10 @@ const void* data_of(PyObject* o, const char* name, at::ScalarType type, const at
     return t.data_ptr();
 }
 
-// The outputs of a call: the caller's dict, or a new one.  `small` outputs of a call (all together `bytes` at the most, up to a megabyte) are tensors over one allocation,
-// which saves 1 us each (a tensor made in Python takes 2.3 us, at::empty 1.1); `make` is a function (shape, dtype, device) -> tensor to be used instead, or None.
+// The outputs of a call: the caller's dict, or a new one with an allocation for each; `make` is a function (shape, dtype, device) -> tensor to be used instead, or None.
 class Outputs {
 public:
-    static constexpr int64_t kShared = 1 << 20, kAlign = 16;
-
-    Outputs(PyObject* given, PyObject* make, const at::Tensor& rows, int64_t bytes) : rows_(rows), make_(make), bytes_(bytes) {
+    Outputs(PyObject* given, PyObject* make, const at::Tensor& rows) : rows_(rows), make_(make) {
         own_ = given == Py_None;
         if (!own_ && !PyDict_Check(given)) {
             PyErr_SetString(PyExc_TypeError, "out must be a dict");
@@ -345,9 +343,9 @@ public:
     Outputs& operator=(const Outputs&) = delete;
 
     // want: the output is due in a new dict; must: it may not be missing from the caller's
-    void* get(const char* name, at::ScalarType type, const Shape& shape, bool want, bool must, bool small = true) {
+    void* get(const char* name, at::ScalarType type, const Shape& shape, bool want, bool must) {
         if (own_) {
-            PyObject* o = want ? fresh(type, shape, small) : Py_NewRef(Py_None);
+            PyObject* o = want ? fresh(type, shape) : Py_NewRef(Py_None);
             const int bad = o ? PyDict_SetItemString(dict_, name, o) : -1;
             void* p = !bad && want ? THPVariable_Unpack(o).data_ptr() : nullptr;
             Py_XDECREF(o);
@@ -373,22 +371,10 @@ public:
     }
 
 private:
-    PyObject* fresh(at::ScalarType type, const Shape& shape, bool small) {
-        if (make_ == Py_None && small && bytes_ <= kShared) {
-            if (!shared_.defined()) shared_ = at::empty({bytes_ + kAlign * 8}, rows_.options().dtype(at::kByte).requires_grad(false));
-            int64_t n = (int64_t)c10::elementSize(type);
-            for (int i = 0; i < shape.dims; ++i) n *= shape.n[i];
-            if (used_ + n <= shared_.numel()) {
-                c10::Storage storage = shared_.storage();
-                at::Tensor t = at::detail::make_tensor<c10::TensorImpl>(std::move(storage), shared_.key_set(), c10::scalarTypeToTypeMeta(type));
-                c10::TensorImpl* impl = t.unsafeGetTensorImpl();
-                impl->set_sizes_contiguous(shape.ref());
-                impl->set_storage_offset(used_ / (int64_t)c10::elementSize(type));
-                used_ += (n + kAlign - 1) / kAlign * kAlign;
-                return THPVariable_Wrap(t);
-            }
-        }
-        if (make_ == Py_None) return THPVariable_Wrap(at::empty(shape.ref(), rows_.options().dtype(type).requires_grad(false)));
+    // (Several outputs over one allocation would save 0.5 us each, but one that is resized would then lie over its neighbours, and torch.save refuses two types over one storage.)
+    PyObject* fresh(at::ScalarType type, const Shape& shape) {
+        if (make_ == Py_None)   // (what at::empty ends in, without its dispatch)
+            return THPVariable_Wrap(at::detail::empty_generic(shape.ref(), c10::cuda::CUDACachingAllocator::get(), c10::DispatchKeySet(c10::DispatchKey::CUDA), type, std::nullopt));
         PyObject* sizes = PyTuple_New(shape.dims);
         if (!sizes) return nullptr;
         for (int i = 0; i < shape.dims; ++i) PyTuple_SET_ITEM(sizes, i, PyLong_FromLongLong(shape.n[i]));
@@ -404,8 +390,6 @@ private:
         return o;
     }
     const at::Tensor& rows_;
-    at::Tensor shared_;
-    int64_t bytes_, used_ = 0;
     PyObject *make_, *dict_ = nullptr;
     bool own_;
 };
@@ -460,7 +444,7 @@ PyObject* token_logprobs(PyObject* const* a) {
     else if (k.R != R) fail("token has the wrong shape");
     const int32_t *index = (const int32_t*)data_of(a[2], "row_index", at::kInt, t, shape_of(n.B, R), true), *token = (const int32_t*)data_of(a[3], "token", at::kInt, t, k.shape, true);
     const c10::cuda::CUDAGuard device(t.device());
-    Outputs out(a[6], a[7], t, (int64_t)n.B * R * 4 * (k.T + 2 + 2 * K));
+    Outputs out(a[6], a[7], t);
     float* logprob = (float*)out.get("logprob", at::kFloat, k.shape, a[3] != Py_None, k.T > 0);
     float* entropy = (float*)out.get("entropy", at::kFloat, shape_of(n.B, R), truth(a[5]), false);
     int32_t* top_token = (int32_t*)out.get("top_token", at::kInt, shape_of(n.B, R, K), K > 0, K > 0);
@@ -486,7 +470,7 @@ PyObject* emitted_logprobs(PyObject* const* a) {
     const int32_t *len = (const int32_t*)len_t.data_ptr(), *last = (const int32_t*)last_t.data_ptr();
     const int32_t *node = (const int32_t*)data_of(a[3], "accepted_node", at::kInt, t, shape_of(n.B, L)), *tok = (const int32_t*)data_of(a[4], "accepted_token", at::kInt, t, shape_of(n.B, L));
     const c10::cuda::CUDAGuard device(t.device());
-    Outputs out(a[8], a[9], t, (int64_t)n.B * (L + 1) * 4 * (4 + 2 * K));
+    Outputs out(a[8], a[9], t);
     int32_t* token = (int32_t*)out.get("token", at::kInt, slots, true, false);
     float *logprob = (float*)out.get("logprob", at::kFloat, slots, true, true), *entropy = (float*)out.get("entropy", at::kFloat, slots, truth(a[7]), false);
     int32_t* top_token = (int32_t*)out.get("top_token", at::kInt, shape_of(n.B, L + 1, K), K > 0, K > 0);
@@ -509,8 +493,8 @@ PyObject* token_logprobs_backward(PyObject* const* a) {
     const int32_t* token = (const int32_t*)data_of(a[2], "token", at::kInt, t, k.shape);
     const float *g = (const float*)data_of(a[3], "grad_logprob", at::kFloat, t, k.shape), *h = (const float*)data_of(a[4], "grad_entropy", at::kFloat, t, shape_of(n.B, n.R), true);
     const c10::cuda::CUDAGuard device(t.device());
-    Outputs out(a[5], a[6], t, (int64_t)n.B * n.R * 4);
-    void* grad = out.get("grad_rows", t.scalar_type(), shape_of(n.B, n.R, n.V), true, true, false);
+    Outputs out(a[5], a[6], t);
+    void* grad = out.get("grad_rows", t.scalar_type(), shape_of(n.B, n.R, n.V), true, true);
     int32_t* status = (int32_t*)out.get("status", at::kInt, shape_of(n.B, n.R), true, true);
     if (n.B == 0) return out.done(Py_NewRef(Py_None));
     const rsd_stream_t s = stream();
@@ -531,7 +515,7 @@ PyObject* row_divergence(PyObject* const* a) {
     check_pair(t, d, n);
     const rsd_rows dr = rows_of(d, false, real(a[1])), tr = rows_of(t, false, real(a[3]));
     const c10::cuda::CUDAGuard device(d.device());
-    Outputs out(a[7], a[8], d, (int64_t)n.B * n.R * 16);
+    Outputs out(a[7], a[8], d);
     const Shape slots = shape_of(n.B, n.R);
     float *kl = (float*)out.get("kl", at::kFloat, slots, truth(a[4]), false), *reverse = (float*)out.get("reverse_kl", at::kFloat, slots, truth(a[5]), false),
           *overlap = (float*)out.get("overlap", at::kFloat, slots, truth(a[6]), false);
@@ -550,8 +534,8 @@ PyObject* row_divergence_backward(PyObject* const* a) {
     const Shape slots = shape_of(n.B, n.R);
     const float *g = (const float*)data_of(a[4], "grad_kl", at::kFloat, d, slots, true), *h = (const float*)data_of(a[5], "grad_reverse_kl", at::kFloat, d, slots, true);
     const c10::cuda::CUDAGuard device(d.device());
-    Outputs out(a[6], a[7], d, (int64_t)n.B * n.R * 4);
-    void* grad = out.get("grad_draft", d.scalar_type(), shape_of(n.B, n.R, n.V), true, true, false);
+    Outputs out(a[6], a[7], d);
+    void* grad = out.get("grad_draft", d.scalar_type(), shape_of(n.B, n.R, n.V), true, true);
     int32_t* status = (int32_t*)out.get("status", at::kInt, slots, true, true);
     if (n.B == 0) return out.done(Py_NewRef(Py_None));
     const rsd_stream_t s = stream();
