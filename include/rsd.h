@@ -71,7 +71,7 @@ enum {
     RSD_ST_TIMEOUT = 32,        /* an on-chip copy of a row did not complete within about a second (a hardware or
                                    driver fault, never a property of the data): the walk of this sequence was
                                    abandoned, accepted_len counts what was accepted before, last_token is -1 */
-    RSD_ST_ZERO_TARGET_PROB = 64, /* scoring: a token with draft mass has target probability 0, so that KL(p||q) is infinite
+    RSD_ST_ZERO_TARGET_PROB = 64, /* scoring: a token with draft mass is missing in the target row, so that KL(p||q) is infinite
                                    (RSD_ST_ZERO_DRAFT_PROB: the other way round, KL(q||p) is infinite) */
     RSD_ST_EMPTY_ROW = 128,     /* scoring: a row without any entry (all -inf, NaN or +inf) */
     RSD_ST_BAD_INDEX = 256      /* scoring: a token >= V or a row index >= the rows there are; it counts as absent */
@@ -359,9 +359,12 @@ int rsd_token_logprobs_backward(const rsd_rows* rows, int B, int R, int V, const
  *   out_reverse_kl  KL(p||q)
  *   out_overlap     sum min(p, q): the probability that a verification accepts one draft (Section 2), 1 - total variation distance
  * each optional [B][R] fp32, at least one of them.  Row r of a sequence's draft is paired with row r of its target (flat node r of a
- * tree), so that the target may have more rows.  Terms with weight 0 are 0; a weight below 2^-126 of its row's largest counts as 0.  A token
- * with mass in one row only makes the divergence from that row infinite (RSD_ST_ZERO_DRAFT_PROB, RSD_ST_ZERO_TARGET_PROB).  NaN
- * and +inf entries count as -inf (RSD_ST_NAN_INPUT); where either row has no entry all three are 0 (RSD_ST_EMPTY_ROW).
+ * tree), so that the target may have more rows.  A term whose weight (q's in KL(q||p), p's in KL(p||q)) is below 2^-126 of its row's largest
+ * is 0.  The other row's logarithm counts in full however small that row's own weight is: a finite entry far below all others gives a large, finite
+ * divergence.  A token is missing in a row where its entry is -inf, NaN or +inf, or so far below the largest that log2(e) times the distance over the
+ * temperature leaves fp32's range; weight in one row where the token is missing in the other makes that divergence infinite
+ * (RSD_ST_ZERO_DRAFT_PROB for KL(q||p), RSD_ST_ZERO_TARGET_PROB for KL(p||q)).  NaN and +inf entries are reported
+ * (RSD_ST_NAN_INPUT); where either row has no entry all three are 0 (RSD_ST_EMPTY_ROW).
  * draft and target must have the same dtype.  The outputs have the same bits in every launch.  status [B][R].
  */
 int rsd_row_divergence(const rsd_rows* draft, const rsd_rows* target, int B, int R, int V, float* out_kl, float* out_reverse_kl,

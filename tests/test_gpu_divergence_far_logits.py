@@ -91,3 +91,14 @@ def test_tiles_of_the_lowest_value(rsd, dtype):
         alone = rsd.rsd_row_divergence_backward(draft, target, g)["grad_draft"]
         assert torch.equal(got["grad_draft"][0], alone[0])
         _check(rsd, draft, target, 2.0, 2.0)                    # (within the range)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_finite_entries_below_every_weight_keep_their_logarithm(rsd, dtype):
+    """-300 beside ordinary entries has a weight far below 2^-126: as a weight it is 0, its logarithm counts where the other row has mass."""
+    draft, target = _pair((2, 2, 5003), dtype)
+    draft[0, :, 17] = -300.0
+    target[1, :, 17] = -300.0
+    draft[:, :, 20], target[:, :, 20] = NEG, -300.0             # no weight: the missing entry does not count
+    out = _check(rsd, draft, target)
+    assert not out["status"].any() and torch.isfinite(out["kl"]).all() and torch.isfinite(out["reverse_kl"]).all()
