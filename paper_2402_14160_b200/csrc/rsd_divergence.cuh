@@ -85,7 +85,7 @@ __device__ __noinline__ CarefulSums add_tile_careful(Words p, Words q, float mp,
         const uint4 pw = i == 0 ? p.w[0] : i == 1 ? p.w[1] : i == 2 ? p.w[2] : p.w[3], qw = i == 0 ? q.w[0] : i == 1 ? q.w[1] : i == 2 ? q.w[2] : q.w[3];
 #pragma unroll
         for (int j = 0; j < P::kEntries; ++j) {
-            const float vp = P::get(pw, j), vq = P::get(qw, j), b = fmaf(vp - zp, kp, -rp), a = fmaf(vq - zq, kq, -rq);
+            const float vp = P::get(pw, j), vq = P::get(qw, j), b = tiles::distance(vp, zp, kp, -rp), a = tiles::distance(vq, zq, kq, -rq);
             const bool in_p = b > kNegInf, in_q = a > kNegInf;
             const float wp = ex2_approx(b), wq = ex2_approx(a), d = in_p && in_q ? a - b : 0.0f;
             if (in_q && !in_p) l.alone_q = fmaxf(l.alone_q, vq);
@@ -168,7 +168,7 @@ __device__ __forceinline__ Totals join(const Sums* sums, int n, float kp, float 
     mp = tiles::warp_max_nan(mp), mq = tiles::warp_max_nan(mq);
     float sp = 0.0f, sq = 0.0f, dp = 0.0f, dq = 0.0f, alone_p = kNegInf, alone_q = kNegInf;
     for (int t = lane; t < n; t += 32) {
-        const float mtp = sums[t].mp, mtq = sums[t].mq, far_p = (mtp - mp) * kp, far_q = (mtq - mq) * kq;
+        const float mtp = sums[t].mp, mtq = sums[t].mq, far_p = tiles::distance(mtp, mp, kp), far_q = tiles::distance(mtq, mq, kq);
         const bool has_p = far_p > kNegInf, has_q = far_q > kNegInf;   // (a tile whose distance leaves fp32's range is missing, like single entries)
         const float bp = has_p ? far_p - tiles::rounded_off(mtp, kp) : 0.0f, bq = has_q ? far_q - tiles::rounded_off(mtq, kq) : 0.0f;
         if (has_p && !has_q) alone_p = fmaxf(alone_p, mtp);
@@ -264,8 +264,8 @@ __device__ __forceinline__ Result result_of(const DivergenceArgs& a, const Smem&
     r.kl_infinite = r.reverse_infinite = false;
     r.log2_sp = r.log2_sq = 0.0f;
     if (r.empty) return r;
-    r.kl_infinite = sm.alone_q && (ordered_to_float(sm.alone_q) - t.mq) * a.k_target >= -126.0f;
-    r.reverse_infinite = sm.alone_p && (ordered_to_float(sm.alone_p) - t.mp) * a.k_draft >= -126.0f;
+    r.kl_infinite = sm.alone_q && tiles::distance(ordered_to_float(sm.alone_q), t.mq, a.k_target) >= -126.0f;
+    r.reverse_infinite = sm.alone_p && tiles::distance(ordered_to_float(sm.alone_p), t.mp, a.k_draft) >= -126.0f;
     r.log2_sp = log2f(t.sp), r.log2_sq = log2f(t.sq);
     return r;
 }
@@ -281,17 +281,19 @@ __device__ __forceinline__ float divergence_of(float d, float s, float other) {
 // log2 of a row's probabilities: v k - c + off in a plain row, (v - m) k - c otherwise; off is what c loses when it is rounded.
 struct LogProb {
     bool plain;
-    float c, off;
-    unsigned long long kk, minus_c, minus_m;
+    float m, k, c, off;                            // (m is 0 in a plain row)
     template <bool PLAIN>
-    __device__ __forceinline__ unsigned long long of(unsigned long long v) const { return fma_f32x2(PLAIN ? v : add_f32x2(v, minus_m), kk, minus_c); }
+    __device__ __forceinline__ unsigned long long of(unsigned long long v) const {
+        if (PLAIN) return fma_f32x2(v, tiles::both(k), tiles::both(-c));
+        return fma_f32x2(fma_f32x2(v, tiles::both(tiles::part_of(k)), tiles::both(-m * tiles::part_of(k))), tiles::both(tiles::scale_of_part(k)), tiles::both(-c));   // (tiles::distance)
+    }
 };
 __device__ __forceinline__ LogProb log_prob(float m, float k, float log2s, bool empty) {
     LogProb l;
     l.plain = tiles::plain_tile(m, k);
+    l.m = l.plain || empty ? 0.0f : m, l.k = k;
     l.c = l.plain ? fmaf(m, k, log2s) : log2s;
     l.off = l.plain ? -(fmaf(m, k, -l.c) + log2s) : 0.0f;
-    l.kk = tiles::both(k), l.minus_c = tiles::both(-l.c), l.minus_m = tiles::both(l.plain || empty ? 0.0f : -m);
     return l;
 }
 
@@ -376,7 +378,7 @@ __device__ __noinline__ void write_wide(const void* draft, const void* target, v
         return v < __builtin_huge_valf() ? v : kNegInf;
     };
     for (int i = first; i < V; i += step) {
-        float x = fmaf(entry(draft, i) - f.mp, f.kp, -f.cp), u = fmaf(entry(target, i) - f.mq, f.kq, -f.cq);
+        float x = tiles::distance(entry(draft, i), f.mp, f.kp, -f.cp), u = tiles::distance(entry(target, i), f.mq, f.kq, -f.cq);
         const double wp = (double)ex2_approx(x) * f.scale_p, wq = (double)ex2_approx(u) * f.scale_q;
         double slope = (wp - wq) * f.g;
         if (REVERSE) {
@@ -423,7 +425,7 @@ __global__ void __launch_bounds__(NW * 32, 24 / NW) divergence_grad_kernel(const
     };
     if (!res.empty && !(lp.plain && lq.plain && tiles::ordinary_factor(c0f) && tiles::ordinary_factor(c1f) && tiles::ordinary_factor(cgf))) {
         WideSlope f;
-        f.mp = lp.plain ? 0.0f : sm.total.mp, f.mq = lq.plain ? 0.0f : sm.total.mq, f.kp = a.k_draft, f.kq = a.k_target, f.cp = lp.c, f.cq = lq.c;
+        f.mp = lp.m, f.mq = lq.m, f.kp = a.k_draft, f.kq = a.k_target, f.cp = lp.c, f.cq = lq.c;
         f.g = (double)g * (double)a.inv_draft_temp, f.h = ht == 0.0f ? 0.0 : (double)h * (double)a.inv_draft_temp;
         f.scale_p = (double)scale_p, f.scale_q = (double)scale_q, f.off = (double)lp.off - (double)lq.off, f.reverse = (double)reverse;
         const int threads = NW * 32;

@@ -59,12 +59,14 @@ __device__ __forceinline__ void tile_sums(uint4 (&w)[kWords], float k, int t, in
         }
         if (m > kNegInf) {
             const bool plain = tiles::plain_tile(m, k);   // (as the join takes it)
-            const unsigned long long minus_m = tiles::both(plain ? 0.0f : -m), ref = tiles::both(plain ? -(m * k) : 0.0f), kk = tiles::both(k);
+            const float half = tiles::part_of(k);
+            const unsigned long long part = tiles::both(half), minus_m = tiles::both(plain ? 0.0f : -m * half), ref = tiles::both(plain ? -(m * k) : 0.0f),
+                                     kk = tiles::both(tiles::scale_of_part(k));
 #pragma unroll
             for (int i = 0; i < kWords; ++i)
                 P::pairs(w[i], [&](unsigned long long v) {
                     float a, b;
-                    split_f32x2(fma_f32x2(add_f32x2(v, minus_m), kk, ref), a, b);
+                    split_f32x2(fma_f32x2(fma_f32x2(v, part, minus_m), kk, ref), a, b);
                     a = fmaxf(a, tiles::kFarBelow), b = fmaxf(b, tiles::kFarBelow);
                     const unsigned long long x = f32x2(ex2_approx(a), ex2_approx(b));
                     s = add_f32x2(s, x);
@@ -114,7 +116,7 @@ __device__ __forceinline__ RowTotals join(const Sums& sums, int n, float k, int 
     for (int t = lane; t < n; t += 32) {
         const float mt = sums.m[t];
         if (mt == kNegInf) continue;
-        const float d = fmaxf((mt - m) * k, tiles::kFarBelow) - tiles::rounded_off(mt, k), f = ex2_approx(d);
+        const float d = fmaxf(tiles::distance(mt, m, k), tiles::kFarBelow) - tiles::rounded_off(mt, k), f = ex2_approx(d);
         s = fmaf(f, sums.s[t], s);
         if (ENTROPY) w = fmaf(f, fmaf(d, sums.s[t], sums.w[t]), w);
     }
@@ -361,7 +363,7 @@ __global__ void __launch_bounds__(NW * 32, 32 / NW) score_rows_kernel(const __gr
     const RowTotals total = total_of_row;
     const bool none = !there || total.m == kNegInf;
     const float lnz = none ? 0.0f : logf(total.s);
-    auto logprob = [&](float v) { return v == kNegInf ? kNegInf : fmaf(v - total.m, a.inv_temp, -lnz); };
+    auto logprob = [&](float v) { return v == kNegInf ? kNegInf : tiles::distance(v, total.m, a.inv_temp, -lnz); };
     if (tid < a.T) {
         if (a.out_logprob) a.out_logprob[slot * a.T + tid] = there && token >= 0 ? logprob(value) : 0.0f;
         if (a.out_token) a.out_token[slot] = there ? token : -1;
@@ -428,7 +430,7 @@ __device__ __forceinline__ Slope slope_of(const RowTotals& total, float G, float
 // The gradient of an entry in 64 bits, and of a row's entries from..to - 1: a weight of 0 makes every finite factor 0, and factors that are not finite reach every entry.
 template <bool ENTROPY>
 __device__ __forceinline__ double wide_slope(float v, float k, const Slope& f) {
-    float x = fmaf(v - f.m, k, -f.c);
+    float x = tiles::distance(v, f.m, k, -f.c);
     if (ENTROPY) x = fmaxf(x, tiles::kNoWeight);
     const double p = (double)ex2_approx(x);
     return p * (ENTROPY ? fma((double)x, f.wide_c1, f.wide_c0) : f.wide_c0);

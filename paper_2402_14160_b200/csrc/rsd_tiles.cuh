@@ -408,6 +408,14 @@ __device__ __forceinline__ float warp_sum_four(float a, float b, float c, float 
     return mine;
 }
 
+// (v - m) k + c.  The difference of two entries may leave fp32's range where its product with k < 1 does not: halves are subtracted there (the same bits otherwise).
+__device__ __forceinline__ float part_of(float k) { return k < 1.0f ? 0.5f : 1.0f; }
+__device__ __forceinline__ float scale_of_part(float k) { return k < 1.0f ? 2.0f * k : k; }
+__device__ __forceinline__ float distance(float v, float m, float k, float c = 0.0f) {
+    const float part = part_of(k);
+    return fmaf(fmaf(v, part, -m * part), scale_of_part(k), c);
+}
+
 // Exponents below this give weights of 0 and may be replaced by it; kLowest: the lowest finite one, where the exponent itself counts.
 constexpr float kFarBelow = -1e30f, kLowest = -3.402823466e38f;
 // The same where an exponent is multiplied by a gradient's factor of at most kMostFactor: their product stays finite, so that a weight of 0 makes it 0.  Rows with larger factors, and

@@ -115,3 +115,17 @@ def test_emitted_tokens_of_masked_rows(rsd, dtype):
     out = rsd.rsd_emitted_logprobs(rows, walked, top_k=5, temperature=0.3)
     sc.check_scores(out, rows, token, 5, 0.3)
     assert not out["status"].any()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [3.0, 1e3, 1e37, 3e38])
+def test_rows_over_the_whole_range(rsd, dtype, T):
+    """Differences of two entries beyond the type's range, at temperatures that bring them back into it."""
+    most = torch.finfo(DT[dtype]).max
+    g = torch.Generator().manual_seed(9)
+    draft, target = ((most * (2 * torch.rand((2, 3, V), generator=g).double() - 1)).to(DT[dtype]).cuda() for _ in range(2))
+    draft[0, 0, 4500:], draft[0, 0, 4000] = -most, most         # a whole tile and more
+    target[0, 1, :4500], target[0, 1, 5000] = -most, most
+    draft[1], target[1] = torch.where(draft[1] > 0, most, -most).to(DT[dtype]), torch.where(target[1] > 0, most, -most).to(DT[dtype])
+    _check_scores(rsd, draft, T)
+    _check_pair(rsd, draft, target, T, T, True)
