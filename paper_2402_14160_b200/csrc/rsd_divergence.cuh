@@ -97,13 +97,15 @@ __device__ __noinline__ CarefulSums add_tile_careful(Words p, Words q, float mp,
 }
 
 // masked: a tile of this warp had entries without mass, so that this one is looked through for them at once.
-// next() reads the warp's next tile into the words' places, ahead of the sums over the warp.
+// next() reads the warp's next tile into the words' places, ahead of the sums over the warp.  What is rare goes straight to the blocks' shared memory, and takes no registers of the loop.
 template <typename T, bool BOTH, typename F>   // BOTH: the sums of weight times difference too
-__device__ __forceinline__ void tile_sums(uint4 (&p)[kWords], uint4 (&q)[kWords], float kp, float kq, int t, int lane, uint32_t blocks, Sums* sums, float& alone_p, float& alone_q,
-                                          bool& bad, bool& masked, F next) {
+__device__ __forceinline__ void tile_sums(uint4 (&p)[kWords], uint4 (&q)[kWords], float kp, float kq, int t, int lane, uint32_t blocks, Sums* sums, Smem& sm,
+                                          bool& masked, F next) {
     using P = tiles::Packed16<T>;
     float mp = tiles::warp_max_nan(P::largest(p)), mq = tiles::warp_max_nan(P::largest(q));
     if (!(mp < __builtin_huge_valf()) || !(mq < __builtin_huge_valf())) {   // NaN or +inf: no entries
+        bool bad = false;
+        if (lane < blocks) tiles::or_at(&sm.status, lane, RSD_ST_NAN_INPUT);
 #pragma unroll
         for (int i = 0; i < kWords; ++i) P::clean(p[i], bad), P::clean(q[i], bad);
         mp = tiles::warp_max_nan(P::largest(p)), mq = tiles::warp_max_nan(P::largest(q));
@@ -143,7 +145,9 @@ __device__ __forceinline__ void tile_sums(uint4 (&p)[kWords], uint4 (&q)[kWords]
             for (int i = 0; i < kWords; ++i) pw.w[i] = p[i], qw.w[i] = q[i];
             const CarefulSums c = add_tile_careful<T>(pw, qw, mp, mq, kp, kq);
             l = {f32x2(c.sp, 0.0f), f32x2(c.sq, 0.0f), f32x2(c.dp, 0.0f), f32x2(c.dq, 0.0f)};
-            alone_p = fmaxf(alone_p, c.alone_p), alone_q = fmaxf(alone_q, c.alone_q);
+            const float alone_p = tiles::warp_max_nan(c.alone_p), alone_q = tiles::warp_max_nan(c.alone_q);
+            if (lane < blocks && alone_p > kNegInf) tiles::max_at(&sm.alone_p, lane, float_to_ordered(alone_p));
+            if (lane < blocks && alone_q > kNegInf) tiles::max_at(&sm.alone_q, lane, float_to_ordered(alone_q));
             halves(1.0f);
         }
     }
@@ -225,17 +229,10 @@ __device__ __forceinline__ bool read_rows(const DivergenceArgs& a, const Pair& w
     };
     load(w.first);
     if (w.blocks > 1) tiles::cluster_wait();
-    float alone_p = kNegInf, alone_q = kNegInf;
-    bool bad = false, masked = false;
+    bool masked = false;
 #pragma unroll 1
     for (int t = w.first; t < w.n_tiles; t += w.step)
-        tile_sums<T, BOTH>(p, q, a.k_draft, a.k_target, t, lane, w.blocks, w.sums, alone_p, alone_q, bad, masked, [&] { load(t + w.step); });
-    if (bad || alone_p > kNegInf || alone_q > kNegInf)
-        for (uint32_t i = 0; i < w.blocks; ++i) {
-            if (bad) tiles::or_at(&sm.status, i, RSD_ST_NAN_INPUT);
-            if (alone_p > kNegInf) tiles::max_at(&sm.alone_p, i, float_to_ordered(alone_p));
-            if (alone_q > kNegInf) tiles::max_at(&sm.alone_q, i, float_to_ordered(alone_q));
-        }
+        tile_sums<T, BOTH>(p, q, a.k_draft, a.k_target, t, lane, w.blocks, w.sums, sm, masked, [&] { load(t + w.step); });
     tiles::row_barrier(w.blocks);
     if (warp == 0) {
         const Totals t = join<BOTH>(w.sums, w.n_tiles, a.k_draft, a.k_target, lane);
@@ -282,11 +279,8 @@ __device__ __forceinline__ float divergence_of(float d, float s, float other) {
 struct LogProb {
     bool plain;
     float m, k, c, off;                            // (m is 0 in a plain row)
-    template <bool PLAIN>
-    __device__ __forceinline__ unsigned long long of(unsigned long long v) const {
-        if (PLAIN) return fma_f32x2(v, tiles::both(k), tiles::both(-c));
-        return fma_f32x2(fma_f32x2(v, tiles::both(tiles::part_of(k)), tiles::both(-m * tiles::part_of(k))), tiles::both(tiles::scale_of_part(k)), tiles::both(-c));   // (tiles::distance)
-    }
+    __device__ __forceinline__ unsigned long long of(unsigned long long v) const { return fma_f32x2(v, tiles::both(k), tiles::both(-c)); }   // of a plain row
+    __device__ __forceinline__ float at(float v) const { return tiles::distance(v, m, k, -c); }
 };
 __device__ __forceinline__ LogProb log_prob(float m, float k, float log2s, bool empty) {
     LogProb l;
@@ -295,6 +289,25 @@ __device__ __forceinline__ LogProb log_prob(float m, float k, float log2s, bool 
     l.c = l.plain ? fmaf(m, k, log2s) : log2s;
     l.off = l.plain ? -(fmaf(m, k, -l.c) + log2s) : 0.0f;
     return l;
+}
+
+template <typename T>
+__device__ __forceinline__ float entry_of(const void* row, int x) {   // -inf where it is none
+    const float v = RowIO<T>::scalar(row, x);
+    return v < __builtin_huge_valf() ? v : kNegInf;
+}
+// The overlap's sums of this warp's tiles where a row is not plain (out of line: the kernel waits for its instructions as it is).
+template <typename T>
+__device__ __noinline__ void overlap_of_far_rows(const void* draft, const void* target, int first, int step, int V, LogProb p, LogProb q, Sums* sums) {
+    constexpr int kTile = tiles::tile_entries<T>(kWords);
+    const int lane = threadIdx.x & 31, n = tiles::tiles_of<T>(V, kWords);
+    for (int t = first; t < n; t += step) {
+        float s = 0.0f;
+        for (int x = t * kTile + lane; x < min((t + 1) * kTile, V); x += 32)
+            s += ex2_approx(fminf(p.at(entry_of<T>(draft, x)), q.at(entry_of<T>(target, x)) + (q.off - p.off)));
+        s = tiles::warp_sum_two(s, 0.0f, lane);
+        if (lane == 0) tiles::store_at(&sums[t].overlap, 0, s);
+    }
 }
 
 template <typename T, bool ALIGNED, bool OVERLAP, int NW>
@@ -316,8 +329,9 @@ __global__ void __launch_bounds__(NW * 32, 32 / NW) divergence_kernel(const __gr
     if constexpr (OVERLAP) {
         const LogProb p = log_prob(sm.total.mp, a.k_draft, res.log2_sp, res.empty), q = log_prob(sm.total.mq, a.k_target, res.log2_sq, res.empty);
         const unsigned long long shift = tiles::both(q.off - p.off);
-        auto sweep = [&](auto plain) {
-            constexpr bool PLAIN = decltype(plain)::value;
+        if (!res.empty && !(p.plain && q.plain)) {
+            overlap_of_far_rows<T>(w.draft.base + w.draft.first, w.target.base + w.target.first, w.first, w.step, a.V, p, q, w.sums);
+        } else if (!res.empty) {
             uint4 pw[kWords], qw[kWords];
             auto load = [&](int t) {
                 if (t < 0) return;
@@ -339,8 +353,8 @@ __global__ void __launch_bounds__(NW * 32, 32 / NW) divergence_kernel(const __gr
 #pragma unroll
                     for (int j = 0; j < P::kEntries / 2; ++j) {
                         float x, y, u, v;
-                        split_f32x2(p.of<PLAIN>(P::pair(pw[i], j)), x, y);
-                        split_f32x2(add_f32x2(q.of<PLAIN>(P::pair(qw[i], j)), shift), u, v);
+                        split_f32x2(p.of(P::pair(pw[i], j)), x, y);
+                        split_f32x2(add_f32x2(q.of(P::pair(qw[i], j)), shift), u, v);
                         s = add_f32x2(s, f32x2(ex2_approx(fminf(x, u)), ex2_approx(fminf(y, v))));
                     }
                 load(t - w.step);
@@ -349,10 +363,6 @@ __global__ void __launch_bounds__(NW * 32, 32 / NW) divergence_kernel(const __gr
                 const float sum = tiles::warp_sum_two(x + y, 0.0f, lane);
                 if (lane == 0) tiles::store_at(&w.sums[t].overlap, 0, sum);
             }
-        };
-        if (!res.empty) {
-            if (p.plain && q.plain) sweep(std::true_type());
-            else sweep(std::false_type());
         }
         tiles::row_barrier(w.blocks);
         if (w.rank == 0 && warp == 0) {
@@ -368,22 +378,18 @@ __global__ void __launch_bounds__(NW * 32, 32 / NW) divergence_kernel(const __gr
 // The gradient of rows that are not plain, or where products of weights and factors might leave fp32's range, in 64 bits: a weight of 0 makes every finite factor 0, and
 // factors that are not finite reach every entry.
 struct WideSlope {
-    float mp, mq, kp, kq, cp, cq;                  // log2 p = (v - mp) kp - cp, but for what the logarithms lost
-    double g, h, scale_p, scale_q, off, reverse;   // weights over the temperature, what the logarithms lost, KL(p||q)
+    LogProb p, q;
+    double g, h, scale_p, scale_q, reverse;        // weights over the temperature, what the logarithms lost as factors, KL(p||q)
 };
 template <typename T, bool REVERSE>
 __device__ __noinline__ void write_wide(const void* draft, const void* target, void* grad, int first, int step, int V, WideSlope f) {
-    auto entry = [](const void* row, int x) {      // -inf where it is none
-        const float v = RowIO<T>::scalar(row, x);
-        return v < __builtin_huge_valf() ? v : kNegInf;
-    };
     for (int i = first; i < V; i += step) {
-        float x = tiles::distance(entry(draft, i), f.mp, f.kp, -f.cp), u = tiles::distance(entry(target, i), f.mq, f.kq, -f.cq);
+        float x = f.p.at(entry_of<T>(draft, i)), u = f.q.at(entry_of<T>(target, i));
         const double wp = (double)ex2_approx(x) * f.scale_p, wq = (double)ex2_approx(u) * f.scale_q;
         double slope = (wp - wq) * f.g;
         if (REVERSE) {
             x = fmaxf(x, tiles::kLowest), u = fmaxf(u, tiles::kLowest);
-            slope += wp * f.h * (0.693147180559945309 * ((double)x - (double)u + f.off) - f.reverse);
+            slope += wp * f.h * (0.693147180559945309 * ((double)x - (double)u + ((double)f.p.off - (double)f.q.off)) - f.reverse);
         }
         tiles::Packed16<T>::store(grad, i, (float)slope);
     }
@@ -425,9 +431,9 @@ __global__ void __launch_bounds__(NW * 32, 24 / NW) divergence_grad_kernel(const
     };
     if (!res.empty && !(lp.plain && lq.plain && tiles::ordinary_factor(c0f) && tiles::ordinary_factor(c1f) && tiles::ordinary_factor(cgf))) {
         WideSlope f;
-        f.mp = lp.m, f.mq = lq.m, f.kp = a.k_draft, f.kq = a.k_target, f.cp = lp.c, f.cq = lq.c;
+        f.p = lp, f.q = lq;
         f.g = (double)g * (double)a.inv_draft_temp, f.h = ht == 0.0f ? 0.0 : (double)h * (double)a.inv_draft_temp;
-        f.scale_p = (double)scale_p, f.scale_q = (double)scale_q, f.off = (double)lp.off - (double)lq.off, f.reverse = (double)reverse;
+        f.scale_p = (double)scale_p, f.scale_q = (double)scale_q, f.reverse = (double)reverse;
         const int threads = NW * 32;
         write_wide<T, REVERSE>(w.draft.base + w.draft.first, w.target.base + w.target.first, grad, (int)w.rank * threads + tid, (int)w.blocks * threads, a.V, f);
         finish();
@@ -437,8 +443,8 @@ __global__ void __launch_bounds__(NW * 32, 24 / NW) divergence_grad_kernel(const
     auto word = [&](const uint4& pw, const uint4& qw) {
         return P::make([&](int i) {
             float x, y, u, v;
-            split_f32x2(lp.of<true>(P::pair(pw, i)), x, y);
-            split_f32x2(lq.of<true>(P::pair(qw, i)), u, v);
+            split_f32x2(lp.of(P::pair(pw, i)), x, y);
+            split_f32x2(lq.of(P::pair(qw, i)), u, v);
             const unsigned long long wp = f32x2(ex2_approx(x), ex2_approx(y)), wq = f32x2(ex2_approx(u), ex2_approx(v));
             const unsigned long long apart = tiles::mul_f32x2(fma_f32x2(wq, minus_ratio, wp), cg);
             if (!REVERSE) return apart;
