@@ -19,7 +19,6 @@ struct ScoreArgs {
     // gradient
     const float *g_logprob, *g_entropy;
     void* grad;
-    int slots;                     // B R
 };
 
 struct DivergenceArgs {

@@ -309,13 +309,13 @@ __device__ __forceinline__ void read_tile(uint4 (&w)[KW], uint32_t at, const Vie
 }
 // Tiles t0 .. t1 - 1 of a row as a block holds them, read by words of another boundary: KW words of a lane, 32 words apart, from entry x0 on, where x0 lies
 // `shift` bytes behind a granule.  Entries outside the row are undefined.
-template <typename T, bool ALIGNED, int KW, int STRIDE = kHeldTile<KW>>   // STRIDE: bytes from tile to tile
+template <typename T, bool ALIGNED, int KW>
 __device__ __forceinline__ void held_words(uint4 (&w)[KW], uint32_t held, const View& v, int t0, int t1, int x0, int V) {
     constexpr int kPerTile = KW * 32;
     const int at = v.first + x0 * (int)sizeof(T), shift = at & 15, local = (at >> 4) - t0 * kPerTile;   // granule of the block
     const int last = (t1 - t0) * kPerTile + (shift == 0 ? -1 : 0) - (KW - 1) * 32;                    // (the granule behind a tile's last one is held with it)
     if (ALIGNED || (local >= 0 && local <= last - 1)) {
-        constexpr int kGap = STRIDE - kPerTile * 16;
+        constexpr int kGap = kHeldTile<KW> - kPerTile * 16;
         const uint32_t a = held + local * 16 + local / kPerTile * kGap;
         if (ALIGNED || shift == 0) {
             // words of one tile, or of two where the lane's words cross into the next one
