@@ -379,7 +379,7 @@ __global__ void __launch_bounds__(NW * 32, 32 / NW) divergence_kernel(const __gr
 // factors that are not finite reach every entry.
 struct WideSlope {
     LogProb p, q;
-    double g, h, scale_p, scale_q, reverse;        // weights over the temperature, what the logarithms lost as factors, KL(p||q)
+    double g, h, scale_p, scale_q, mean;           // weights over the temperature
 };
 template <typename T, bool REVERSE>
 __device__ __noinline__ void write_wide(const void* draft, const void* target, void* grad, int first, int step, int V, WideSlope f) {
@@ -389,7 +389,7 @@ __device__ __noinline__ void write_wide(const void* draft, const void* target, v
         double slope = (wp - wq) * f.g;
         if (REVERSE) {
             x = fmaxf(x, tiles::kLowest), u = fmaxf(u, tiles::kLowest);
-            slope += wp * f.h * (0.693147180559945309 * ((double)x - (double)u + ((double)f.p.off - (double)f.q.off)) - f.reverse);
+            slope += wp * f.h * 0.693147180559945309 * ((double)x - (double)u + ((double)f.p.off - (double)f.q.off) - f.mean);
         }
         tiles::Packed16<T>::store(grad, i, (float)slope);
     }
@@ -413,11 +413,12 @@ __global__ void __launch_bounds__(NW * 32, 24 / NW) divergence_grad_kernel(const
     const float g = a.g_kl ? a.g_kl[w.slot] : 0.0f, h = REVERSE ? a.g_reverse[w.slot] : 0.0f;
     const Result res = result_of(a, sm);
     const float gt = res.empty ? 0.0f : g * a.inv_draft_temp, ht = res.empty || (REVERSE && res.reverse_infinite) ? 0.0f : h * a.inv_draft_temp;
-    const LogProb lp = log_prob(sm.total.mp, a.k_draft, res.log2_sp, res.empty), lq = log_prob(sm.total.mq, a.k_target, res.log2_sq, res.empty);
-    const float scale_p = ex2_approx(lp.off), scale_q = ex2_approx(lq.off);
-    // gt (p - q) + p ht (ln 2 (log2 p - log2 q) - KL(p||q)); rows that are equal give 0
-    const float reverse = REVERSE && ht != 0.0f ? 0.69314718f * (__fdividef(sm.total.dp, sm.total.sp) * (1.0f / kUnit) + res.log2_sq - res.log2_sp) : 0.0f;
-    const float c1f = ht * 0.69314718f * scale_p, c0f = fmaf(ht * 0.69314718f, lp.off - lq.off, -ht * reverse) * scale_p, cgf = gt * scale_p;
+    // p = 2^x scale_p with x relative to the row's largest entry, q = 2^u scale_q alike; then  ln p - ln q - KL(p||q) = ln 2 (x - u - sum p (x - u)),  where no term is as large as ln V.
+    // Rows that are equal give 0.
+    const LogProb lp = log_prob(sm.total.mp, a.k_draft, 0.0f, res.empty), lq = log_prob(sm.total.mq, a.k_target, 0.0f, res.empty);
+    const float scale_p = ex2_approx(lp.off) / sm.total.sp, scale_q = ex2_approx(lq.off) / sm.total.sq;
+    const float mean = REVERSE && ht != 0.0f ? sm.total.dp / sm.total.sp * (1.0f / kUnit) : 0.0f;
+    const float c1f = ht * 0.69314718f * scale_p, c0f = c1f * (lp.off - lq.off - mean), cgf = gt * scale_p;
     char* const grad = (char*)a.grad + w.slot * a.V * (int64_t)sizeof(T);
     const int head = ALIGNED ? 0 : (int)((uintptr_t)grad & 15u) / (int)sizeof(T);   // entries between the boundary and the gradient's first one
     auto finish = [&] {
@@ -433,13 +434,13 @@ __global__ void __launch_bounds__(NW * 32, 24 / NW) divergence_grad_kernel(const
         WideSlope f;
         f.p = lp, f.q = lq;
         f.g = (double)g * (double)a.inv_draft_temp, f.h = ht == 0.0f ? 0.0 : (double)h * (double)a.inv_draft_temp;
-        f.scale_p = (double)scale_p, f.scale_q = (double)scale_q, f.reverse = (double)reverse;
+        f.scale_p = (double)scale_p, f.scale_q = (double)scale_q, f.mean = (double)mean;
         const int threads = NW * 32;
         write_wide<T, REVERSE>(w.draft.base + w.draft.first, w.target.base + w.target.first, grad, (int)w.rank * threads + tid, (int)w.blocks * threads, a.V, f);
         finish();
         return;
     }
-    const unsigned long long c0 = tiles::both(c0f), c1 = tiles::both(c1f), cg = tiles::both(cgf), minus_ratio = tiles::both(-__fdividef(scale_q, scale_p)), minus_one = tiles::both(-1.0f);
+    const unsigned long long c0 = tiles::both(c0f), c1 = tiles::both(c1f), cg = tiles::both(cgf), minus_ratio = tiles::both(-scale_q / scale_p), minus_one = tiles::both(-1.0f);
     auto word = [&](const uint4& pw, const uint4& qw) {
         return P::make([&](int i) {
             float x, y, u, v;
