@@ -286,7 +286,7 @@ __device__ __forceinline__ LogProb log_prob(float m, float k, float log2s, bool 
     LogProb l;
     l.plain = tiles::plain_tile(m, k);
     l.m = l.plain || empty ? 0.0f : m, l.k = k;
-    l.c = l.plain ? fmaf(m, k, log2s) : log2s;
+    l.c = l.plain ? __fmaf_ru(m, k, log2s) : log2s;   // (rounded up: no weight is above 1, so that its product with any finite number is finite)
     l.off = l.plain ? -(fmaf(m, k, -l.c) + log2s) : 0.0f;
     return l;
 }
