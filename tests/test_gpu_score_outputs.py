@@ -62,3 +62,26 @@ def test_outputs_saved_and_kept(rsd, tmp_path):
     torch.save({k: v for k, v in out.items()}, tmp_path / "out.pt")
     back = torch.load(tmp_path / "out.pt")
     assert all(torch.equal(back[k], out[k]) for k in out)
+
+
+def test_outputs_of_no_sequences_and_in_a_captured_graph(rsd):
+    rows = sc.random_rows((3, 5, 2000), torch.bfloat16, 2.0, 1)
+    token = torch.randint(0, 2000, (3, 5), generator=torch.Generator().manual_seed(2), dtype=torch.int32).cuda()
+    one = torch.ones((3, 5)).cuda()
+
+    def every(r, t, w):
+        return [rsd.rsd_token_logprobs(r, t, top_k=3), rsd.rsd_token_logprobs_backward(r, t, w), rsd.rsd_row_divergence(r, r), rsd.rsd_row_divergence_backward(r, r, w, w)]
+
+    for out in every(rows[:0], token[:0], one[:0]):
+        assert all(v.shape[:2] == (0, 5) and v.is_cuda for v in out.values())
+    want = every(rows, token, one)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = every(rows, token, one)
+    for out in got:
+        for v in out.values():
+            v.fill_(3)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a[k], b[k]) for a, b in zip(got, want) for k in b)
