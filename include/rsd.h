@@ -345,7 +345,8 @@ int rsd_emitted_logprobs(const rsd_rows* target, int B, int num_nodes, int V, in
  *   ( sum_{t: token_t = x} g_t - p_x (sum_t g_t + h (ln p_x + H)) ) / T
  * The normalisers are taken from the row again, so that nothing has to be kept from the forward call.  A token given twice counts twice,
  * an absent one not at all; entries without probability get what the formula gives at p_x = 0; a row without entries gets 0 throughout.
- * A weight of a token that is there, or of the entropy, that is NaN or infinite leaves no finite entry in its row's gradient; finite ones count in full.
+ * A weight of a token that is there, or of the entropy, that is NaN or infinite leaves no finite entry in its row's gradient; finite ones, whose
+ * sum in fp32 is finite too, count in full.
  *   rows [B][R][V];  token [B][R][T], 1 <= T <= RSD_MAX_K;  grad_logprob [B][R][T], grad_entropy optional [B][R], fp32
  *   grad_rows    [B][R][V] dense, the rows' element type, rounded once; may not overlap the rows
  *   status       [B][R]

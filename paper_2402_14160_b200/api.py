@@ -322,7 +322,7 @@ def rsd_token_logprobs(rows: torch.Tensor, token: Optional[torch.Tensor] = None,
                        want_entropy: bool = True, temperature: float = 1.0, out: Optional[dict] = None):
     """rows [B, N, V], token [B, R] or [B, R, T] int32 (-1: absent) or None, row_index [B, R] int32 or None (slot r is row r) -> dict(logprob of
     token's shape, entropy [B, R], top_token and top_logprob [B, R, top_k], status [B, R]); None where not asked for.  logprob is 0 for an
-    absent token or slot.  For gradients see rsd_token_logprobs_backward."""
+    absent token or slot.  The outputs carry no autograd history: gradients are a call of their own, rsd_token_logprobs_backward."""
     return (_native or _bind()).token_logprobs(rows, temperature, row_index, token, top_k, want_entropy, out, _make())
 
 
@@ -346,7 +346,7 @@ def rsd_token_logprobs_backward(rows: torch.Tensor, token: torch.Tensor, grad_lo
 def rsd_row_divergence(draft: torch.Tensor, target: torch.Tensor, *, want_kl: bool = True, want_reverse_kl: bool = True, want_overlap: bool = True,
                        draft_temperature: float = 1.0, target_temperature: float = 1.0, out: Optional[dict] = None):
     """draft [B, R, V], target [B, >= R, V] -> dict(kl = KL(target || draft), reverse_kl = KL(draft || target), overlap = sum min(p, q), status
-    [B, R]); None where not asked for.  For gradients see rsd_row_divergence_backward."""
+    [B, R]); None where not asked for.  The outputs carry no autograd history: gradients are a call of their own, rsd_row_divergence_backward."""
     return (_native or _bind()).row_divergence(draft, draft_temperature, target, target_temperature, want_kl, want_reverse_kl, want_overlap, out, _make())
 
 

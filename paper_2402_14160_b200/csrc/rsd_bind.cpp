@@ -371,7 +371,7 @@ public:
     }
 
 private:
-    // (Several outputs over one allocation would save 0.5 us each, but one that is resized would then lie over its neighbours, and torch.save refuses two types over one storage.)
+    // (Several outputs over one allocation would save 0.2 us each, but one that is resized would then lie over its neighbours, and torch.save refuses two types over one storage.)
     PyObject* fresh(at::ScalarType type, const Shape& shape) {
         if (make_ == Py_None)   // (what at::empty ends in, without its dispatch)
             return THPVariable_Wrap(at::detail::empty_generic(shape.ref(), c10::cuda::CUDACachingAllocator::get(), c10::DispatchKeySet(c10::DispatchKey::CUDA), type, std::nullopt));

@@ -6,8 +6,9 @@
 // so both come from one pass with one exponential per entry and row; what cancels is of the size of 1, not of the size of a logit.
 // The overlap sum min(p, q) needs the normalisers first: a second pass (from L2) with one exponential per pair, 2^min(log2 p, log2 q).
 //
-// 7296 pairs of 32,000 bf16: 260 us (floor 143), KL alone 150 (0.95 of the measured copy bandwidth).  With the overlap three exponentials a pair of entries and 26,000 warp
-// instructions a pair of rows keep the special-function unit and the issue slots 60 to 63 % busy; at their full rates either would take 158 us.  fp32 pairs 375 of 7000 (floor 273).
+// 7296 pairs of 32,000 bf16: 280 us back to back (259 below the power limit; floor 143); 7000 pairs without the overlap 149 (floor 137).  With it three exponentials a pair of entries and
+// 26,400 warp instructions a pair of rows keep the special-function unit and the issue slots 61 to 63 % busy.  7000 fp32 pairs 375 (floor 273).  Rows that are not plain: 4096 pairs 258 us
+// (150).
 // Slower: the rows held in shared memory, which takes clusters of two blocks (401), halves of the next tile read in between (its conditions cost more than the wait), a prefetch of
 // whole rows into L2 (a tenth), edges of rows out of line (3 %).
 #pragma once
@@ -398,9 +399,9 @@ __device__ __noinline__ void write_wide(const void* draft, const void* target, v
 // d KL(q||p) / dv_x = (p_x - q_x) / T,   d KL(p||q) / dv_x = p_x (log p_x - log q_x - KL(p||q)) / T,   v the draft row, T its temperature.
 // A row whose KL(p||q) is infinite has no gradient of it.  Words of the gradient are written on their own 16-byte boundaries.
 //
-// 4096 pairs of 32,000 bf16, KL(q||p): 160 us (floor 120): four exponentials a pair of entries, the special-function unit 72 % busy.  (A quarter of the second sweep's exponentials by a
+// 4096 pairs of 32,000 bf16, KL(q||p): 180 us back to back (167 below the power limit; floor 120): four exponentials a pair of entries, the special-function unit 73 % busy.  (A quarter of the second sweep's exponentials by a
 // polynomial on the multiplying pipe: 2 % faster with KL(q||p) alone, 3 % slower with both.)  fp32 pairs are bound by memory: where the pairs under way do not stay in L2 beside the
-// gradient's words they are read twice (7000 pairs of 32,000: 540 us, floor 410; 192 of 128,000 with both divergences 77, floor 45).
+// gradient's words they are read twice (7000 pairs of 32,000: 535 us, floor 410; 192 of 128,000 with both divergences 77, floor 45).
 template <typename T, bool ALIGNED, bool REVERSE, int NW>
 __global__ void __launch_bounds__(NW * 32, 24 / NW) divergence_grad_kernel(const __grid_constant__ DivergenceArgs a) {
     using P = tiles::Packed16<T>;

@@ -286,8 +286,8 @@ __device__ __forceinline__ bool slot_of(const ScoreArgs& a, int64_t slot, int64_
 
 // Tiles of a row are dealt to the warps of its blocks in turn: tile t to warp t / blocks mod NW of block t mod blocks.
 //
-// 14,592 rows of 32,000 bf16 with 8 tokens and the entropy: 142 us = 6.6 TB/s, the measured copy bandwidth, as long as the chip is below its power limit; called without a
-// pause it draws 1000 W, the SMs go down to 1.6 GHz and it takes 160 to 170.  Issue slots 54 % busy, special-function unit 68 % (7540 warp instructions a row, 4650 of them
+// 14,592 rows of 32,000 bf16 with 8 tokens and the entropy: 170 us = 5.5 TB/s back to back, where the chip draws 1000 W and the SMs go down to 1.6 GHz (142 us, the measured copy
+// bandwidth, as long as it is below its power limit).  Issue slots 54 % busy, special-function unit 67 % (7560 warp instructions a row, 4650 of them
 // the least that unpacking, bounding, scaling, exponentials and the two sums take).  Few rows are bound by what follows on each other: one row of 32,000 3.9 us, with five likeliest
 // tokens 6.5; 2560 of them 39 and 49 us (floor 25), where the rows that start last have the chip to themselves.
 template <typename T, bool ALIGNED, bool TOP, int NW>
@@ -397,10 +397,10 @@ __global__ void __launch_bounds__(NW * 32, 32 / NW) score_rows_kernel(const __gr
 // A block has consecutive tiles of its row and keeps them in shared memory for the second sweep (read again from L2, the
 // gradient's own words pushed two thirds of the rows out to memory); words of the gradient are written on their own 16-byte boundaries.
 //
-// 8192 rows of 32,000 bf16 with an entropy term: 210 us = 5.0 TB/s read and written, 0.76 of the measured copy bandwidth (sustained, at the power limit, 228; 9 us of it
-// are the limits under which masked entries get 0 whatever the factors).  Three rows an SM are what
-// shared memory holds, 24 warps; two exponentials an entry keep the special-function unit 60 % busy, and the warps wait for each other at the two barriers (15 % of
-// the stalls) and for the unit's queue.  Slower: blocks that stay for several rows and ask for the next one early (224: without arithmetic 180 against 159), 4 warps a row (225).
+// 8192 rows of 32,000 bf16 with an entropy term: 221 us = 4.7 TB/s read and written back to back, 0.72 of the measured copy bandwidth (201 below the power limit).  Three rows an SM are what
+// shared memory holds, 24 warps; two exponentials an entry keep the special-function unit 59 % busy, and the warps wait for each other at the two barriers (15 % of
+// the stalls) and for the unit's queue.  Slower: blocks that stay for several rows and ask for the next one early (by 7 %: without arithmetic 180 us against 159), 4 warps a row (by 7 %).
+// Rows that are not plain, or whose factors are not ordinary, are written entry by entry in 64 bits (4096 rows 343 us, the others 105).
 struct Slope {                     // gradient of an entry without a token: p (c0 + c1 log2 p),   log2 p = (v - m) k - c, m = 0 in a plain row
     float m, c, c0, c1, inv_temp;
     double wide_c0, wide_c1;       // the factors of rows that are not plain, or where products in fp32 might leave its range

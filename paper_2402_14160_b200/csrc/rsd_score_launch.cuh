@@ -11,8 +11,8 @@
 namespace rsd {
 
 // Blocks that share a row: few rows leave most of the chip idle, so that their tiles are dealt to the blocks of a cluster, up to three blocks an SM and as long as
-// every warp has a tile.  (us a call, 1 / 2 / 4 / 8 blocks: likeliest 5 of 1 / 100 / 200 / 400 rows of 128,000 bf16 14.4 / 10.8 / 8.9 / 7.3, 16.5 / 14.0 / 12.9 / 17.1,
-// 20.9 / 18.1 / 23.4 / 28.3, 26.3 / 31.0 / 35.9 / 49.3; divergence of 37 pairs of 32,000 fp32 19.6 / 14.0 / 10.6 / 9.3.)
+// every warp has a tile.  (us a call, 1 / 2 / 4 / 8 blocks: likeliest 5 of 1 / 100 / 200 / 400 rows of 128,000 bf16 14.7 / 10.7 / 8.9 / 7.6, 16.9 / 14.4 / 13.7 / 18.1,
+// 20.9 / 18.2 / 23.7 / 28.9, 26.5 / 31.4 / 36.8 / 50.3; divergence of 37 pairs of 32,000 fp32 17.6 / 13.2 / 10.6 / 9.2.)
 inline int row_blocks(unsigned slots, int n_tiles, int warps) {
     const int sms = rsd_host::sm_count();
     int blocks = 1;
@@ -26,8 +26,8 @@ void launch_rows(void (*kernel)(A), unsigned slots, int blocks, int threads, siz
 
 // Warps per row where a row has one block.  As many as leave all rows resident at 32 warps an SM; rows beyond that take turns, and long turns of few warps leave SMs
 // idle at the end where short ones of many warps pay for their barriers.  (us, 1 / 2 / 4 / 8 warps, bf16 without likeliest tokens: 300 / 700 / 1500 / 7000 rows of 32,000
-// 18.3 / 11.8 / 8.6 / 8.0, 21.2 / 14.9 / 12.5 / 13.7, 25.1 / 22.3 / 22.1 / 21.5, 80.6 / 73.4 / 71.3 / 79.2; 7000 of 8000 23.4 / 24.3 / 27.5 / 42.9; with the
-// likeliest 5, which warps spend more time apart on, 7000 of 32,000 101 / 93 / 97 / 115; 3000 of 128,000 fp32 410 / 307 / 270 / 233.)
+// 19.8 / 12.4 / 8.9 / 8.5, 21.8 / 15.1 / 12.6 / 13.7, 25.6 / 22.2 / 21.4 / 21.4, 82.8 / 74.3 / 71.5 / 79.9; 7000 of 8000 23.7 / 24.7 / 27.8 / 43.6; with the
+// likeliest 5, which warps spend more time apart on, 7000 of 32,000 104 / 94 / 97 / 116; 3000 of 128,000 fp32 218 / 266 / 222 / 220.)
 inline int score_warps(unsigned slots, int n_tiles, bool top) {
     const int sms = rsd_host::sm_count();
     const int most = n_tiles >= 8 ? 8 : n_tiles >= 4 ? 4 : n_tiles >= 2 ? 2 : 1;
@@ -63,7 +63,7 @@ void launch_score_of(bool aligned, unsigned slots, const ScoreArgs& a, cudaStrea
 }
 
 // Gradients of scores: blocks keep their tiles in shared memory, as few blocks a row as leave three of them on an SM (more for few rows).  Short rows have fewer warps (us, 2 / 4 / 8 warps,
-// 7000 bf16 rows of 1500 / 8000 / 32,000: 36 / 59 / 131, 55 / 57 / 90, 262 / 194 / 173).
+// 7000 bf16 rows of 1500 / 8000 / 32,000: 41 / 71 / 129, 56 / 60 / 94, 271 / 197 / 175).
 constexpr int kHeldBytes = 68 * 1024, kMostHeldBytes = 200 * 1024;
 template <typename T, bool ALIGNED, bool ENTROPY, int NW>
 void launch_score_grad_as(unsigned slots, int blocks, const ScoreArgs& a, cudaStream_t s) {
@@ -92,8 +92,10 @@ void launch_score_grad_of(bool aligned, unsigned slots, const ScoreArgs& a, cuda
     }
 }
 
-// Divergences: short rows have fewer warps (us, 2 / 4 / 8 warps: 7000 pairs of 1500 bf16 48 / 58 / 99, of 8000 fp32 140 / 115 / 137, of 32,000 bf16 284 / 291 / 293), and so
-// have many pairs of which no second sweep is asked for (KL alone, 700 / 7000 pairs of 32,000 bf16 32 / 24 / 25, 170 / 164 / 176).
+// Divergences: short rows have fewer warps (us, 2 / 4 / 8 warps: 7000 pairs of 1500 bf16 47 / 61 / 106, of 8000 fp32 111 / 117 / 153), long ones eight, which reads them again from L2
+// (7000 pairs of 32,000 fp32 491 / 442 / 401, bf16 257 / 258 / 260).  Where no second sweep is asked for, many pairs have four (KL alone, 700 / 7000 pairs of 32,000 bf16
+// 33 / 24 / 25, 152 / 148 / 159).  How many blocks are resident is not looked at: a little more than a wave of them (640 pairs of 32,001 bf16 65 / 44 / 46, 700 of 32,000 56 / 42 / 46)
+// would be faster with four warps, two waves (1300 pairs 70 / 66 / 59) are not.
 inline int divergence_warps(unsigned slots, int n_tiles, bool one_sweep) {
     const int sms = rsd_host::sm_count();
     if (n_tiles <= 3) return 2;
@@ -123,8 +125,9 @@ void launch_divergence_of(bool aligned, unsigned slots, const DivergenceArgs& a,
 }
 
 // Gradients of divergences read their rows twice, the second time from L2, which does not hold the pairs under way beside the gradient's words where they are long: those are shared by two or four
-// blocks, so that fewer are under way at a time (us, 1 / 2 / 4 / 8 blocks: 1000 pairs of 32,000 fp32 91 / 89 / 108 / 150, of 60,000 fp32 180 / 159 / 159 / 201, of 128,000 bf16
-// 193 / 179 / 184 / 229, of 128,000 fp32 390 / 355 / 328 / 337; 5000 of 60,000 bf16 387 / 405 / 506 / 713).
+// blocks, so that fewer are under way at a time (us, 1 / 2 / 4 / 8 blocks: 1000 pairs of 32,000 fp32 92 / 90 / 108 / 149, of 60,000 fp32 182 / 159 / 161 / 203, of 128,000 bf16
+// 191 / 177 / 183 / 228, of 128,000 fp32 390 / 357 / 325 / 328; 5000 of 60,000 bf16 386 / 412 / 506 / 702).  The bytes under way are taken as those of three pairs an SM, or of all pairs if there
+// are fewer, over the blocks a pair; between one and three pairs an SM that is too little (192 pairs of 128,000 fp32 88 / 73 / 67 / 72, and it takes two blocks).
 constexpr int64_t kReadAgainBytes = 120 * 1000 * 1000;
 template <typename T, bool ALIGNED, bool REVERSE, int NW>
 void launch_divergence_grad_as(unsigned slots, int blocks, const DivergenceArgs& a, cudaStream_t s) {
